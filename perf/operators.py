@@ -169,14 +169,14 @@ def _prepare_cache(case, seed):
 
 
 def _attend(s):
-    case, n, table = s["case"], s["n"], s["table"].long()
+    case, n, table = s["case"], s["n"], s["table"]
     if own:
-        s["ctx"].kv_attend(layer=0, batch=case["batch"], q=s["q"], out=s["out"], n_tokens=n, page_table=s["table"], max_pages=table.shape[1],
+        s["ctx"].kv_attend(layer=0, batch=case["batch"], q=s["q"], out=s["out"], n_tokens=n, page_table=table, max_pages=table.shape[1],
                            max_kv_len=s["longest"], track=s["track"], decay=case["decay"], position=s["position"], workspace=s["workspace"])
         return {"out": s["out"], "weight": s["track"][..., 0].view(torch.float32), "position": s["track"][..., 1]}
     batch, n_kv, d = case["batch"], case["n_kv"], case["d"]
     group = case["n_q"] // n_kv
-    page = table.clamp(min=0)
+    page = table.long().clamp(min=0)
     kv = s["view"][page // s["ppb"], 0, :, page % s["ppb"]].float()              # [batch, page, K or V, KV head, slot, head size]
     k, v = (kv[:, :, i].transpose(1, 2).reshape(batch * n_kv, -1, d) for i in (0, 1))
     q = (s["q"] / math.sqrt(d)).view(batch * n_kv, group, d)
