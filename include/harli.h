@@ -290,6 +290,123 @@ int32_t harli_decode_tiled_min_batch(void);
 size_t harli_decode_step_static_bytes(const harli_ctx* c, int32_t batch, int32_t max_kv_len);
 
 /* ======================================================================== *
+ * A KV cache inside a budget (Sec. 4.4: inference memory under pressure).  The attention of a step can add up, for every
+ * cached token and KV head, the weight the token receives; tokens that receive little can then leave the cache, in every
+ * layer and KV head by a choice of its own.  What stays moves together, so that the pages behind the kept length can go
+ * back to the pool.
+ *   record  = (accumulated weight, rotary position) of one token in one KV head of one layer.  Records lie in the caller's
+ *             array [n_layers][page ids of the pool][n_kv_heads][page_tokens], found through the page table like keys and
+ *             values (page ids: 0 .. harli_pool_stats_t.n_chunks * pages_per_block - 1).
+ * These calls take their scratch memory from the caller and use nothing of the context that a step in another stream
+ * writes: calls on different streams may overlap when their page tables share no page and their workspaces are apart.  In
+ * one call, too, every page belongs to one sequence: no page id appears twice in the table.  They can be captured
+ * into a HIP graph (the host values in the structs are part of the capture).
+ * ======================================================================== */
+typedef struct {
+  float weight;
+  int32_t position;
+} harli_kv_record;
+
+typedef struct {
+  harli_kv_record* records; /* device, 16-byte aligned; NULL (harli_kv_attend only): nothing is recorded */
+  float decay;              /* 0..1: what a step leaves of the weight that a token had (1: weights add up, 0: the last step's) */
+  const int32_t* position;  /* device [batch]: rotary position of the newest token, that is, how many tokens the sequence has
+                             * had before it, those that have left the cache included; NULL: its index in the cache */
+  void* workspace;          /* device, 256-byte aligned: harli_kv_attend_workspace_bytes(c, batch, max_kv_len) */
+  size_t workspace_bytes;
+} harli_tracking;
+
+/* Attention of one new token per sequence over one layer's cache, the newest token's key and value among it:
+ *   P_h = softmax_j(q_h . k_j / sqrt(head_dim)),  out_h = sum_j P_hj v_j                      for j < n = n_tokens[b]
+ *   weight_j <- decay * weight_j + sum of P_hj over the query heads h of the KV head           for j < n - 1
+ *   the record of token n - 1 is written anew: (sum of P_h,n-1, position)
+ * n = 0: out is zero and no record changes.  Records of other tokens are left as they are.  With decay = 0 the weights that
+ * were there are not looked at.  q is already rotated; keys and values are found as harli_decode_step leaves them.  A token of
+ * a page id outside the pool (or -1) gets no weight and is reported by harli_ctx_check, as is a sequence longer than max_kv_len
+ * (rounded up to whole chunks of 128 or 256 tokens) or its table row, whose further tokens are not seen. */
+typedef struct {
+  int32_t batch;              /* 1..cfg.max_batch */
+  int32_t layer;
+  const float* q;             /* device [batch, n_q_heads, head_dim], 16-byte aligned */
+  float* out;                 /* device [batch, n_q_heads, head_dim], 16-byte aligned */
+  const int32_t* n_tokens;    /* device [batch] */
+  const int32_t* page_table;  /* device [batch, max_pages] */
+  int32_t max_pages;
+  int32_t max_kv_len;         /* host-known upper bound of n_tokens[b], 1..cfg.max_seq_len */
+  harli_tracking track;
+} harli_attend_batch;
+
+harli_status harli_kv_attend(harli_ctx* c, const harli_attend_batch* b, void* hip_stream);
+/* Workspace of harli_kv_attend and harli_decode_step_tracked (host arithmetic; 0 for bad arguments). */
+size_t harli_kv_attend_workspace_bytes(const harli_ctx* c, int32_t batch, int32_t max_kv_len);
+
+/* harli_decode_step with every layer's attention as in harli_kv_attend (n = kv_len[b] + 1), the rotary embedding of the new
+ * tokens at t->position.  t->records is required.  After an eviction kv_len[b] counts what is cached and position[b] goes on. */
+harli_status harli_decode_step_tracked(harli_ctx* c, const harli_decode_batch* b, const harli_tracking* t, void* hip_stream);
+
+/* Records of tokens that arrive from elsewhere (a prompt's): (0, j) for j < n_tokens[b], in every layer and KV head. */
+typedef struct {
+  int32_t batch;              /* 1..cfg.max_batch */
+  const int32_t* n_tokens;    /* device [batch] */
+  const int32_t* page_table;  /* device [batch, max_pages] */
+  int32_t max_pages;
+  int32_t max_kv_len;         /* host-known upper bound of n_tokens[b] */
+  harli_kv_record* records;
+} harli_record_batch;
+harli_status harli_kv_record_init(harli_ctx* c, const harli_record_batch* b, void* hip_stream);
+
+/* Eviction: sequence b goes from n = n_tokens[b] to min(n, max(keep[b], 0)) tokens, each layer and KV head for itself.  Tokens rank
+ * by (protected, weight, lower slot): protected are those with record position < sink or >= position[b] - recent, a weight that
+ * is NaN ranks below every other, and among protected tokens only the slot counts.  The best `keep` stay.  Of them, those in
+ * slots >= keep move, in order, to the slots < keep that fell free, in order: key, value and record.  Nothing else is written:
+ * slots from keep on hold what they held.  Keys keep the rotation they have, and attention does not ask for the order of tokens.
+ * A sequence that already fits is left alone.  A token of a bad page id ranks last and is reported by harli_ctx_check, as is a
+ * sequence longer than max_kv_len or its table row, which is left alone. */
+typedef struct {
+  int32_t batch;              /* 1..cfg.max_batch */
+  const int32_t* n_tokens;    /* device [batch]: tokens cached */
+  const int32_t* keep;        /* device [batch] */
+  const int32_t* position;    /* device [batch]: position of the token that comes next, or NULL: n_tokens */
+  const int32_t* page_table;  /* device [batch, max_pages] */
+  int32_t max_pages;
+  int32_t max_kv_len;         /* host-known upper bound of n_tokens[b], 1..cfg.max_seq_len, at most 2^18 */
+  int32_t sink, recent;       /* >= 0 */
+  harli_kv_record* records;
+  int32_t* n_left;            /* device [batch]: tokens cached afterwards, or NULL; not n_tokens, keep or position */
+} harli_evict_batch;
+harli_status harli_kv_evict(harli_ctx* c, const harli_evict_batch* b, void* hip_stream);
+
+/* ======================================================================== *
+ * A token per row of logits, from random numbers the caller gives (what a service needs in place of next_token).
+ * Row b, its tokens in the order of (higher logit, lower index), weights w_i = exp((logit_i - max) / temperature) in 64 bits:
+ *   top-k   keeps the first k;
+ *   top-p   keeps, of those, each one for which the weights before it add up to less than p times the weight of the k;
+ *   min-p   keeps w_i >= min_p (times the largest weight, which is 1);
+ *   token   = the first index i, by index, at which the kept weights up to i add up to more than uniform times their sum.
+ * The first token in order always stays.  Weights are held in fixed point with 62 bits for a row's sum: a weight below 2^-38 or less
+ * (2^-44 at 152064 tokens) of the largest may be never drawn, and the result does not depend on how the work was split.
+ * temperature <= 0 or NaN: the first token in order.  A logit of -inf or NaN is never drawn; several of +inf share the row.
+ * A row without a token that can be drawn gets token -1, logprob -inf.
+ * ======================================================================== */
+typedef struct {
+  int32_t batch;             /* >= 1 */
+  int32_t vocab;             /* 1..2^24 */
+  const float* logits;       /* device, row b at logits + b * ld */
+  int64_t ld;                /* >= vocab */
+  const float* uniform;      /* device [batch], [0, 1): below 0 or NaN counts as 0, from 1 on draws the last */
+  const float* temperature;  /* device [batch] or NULL: 1 */
+  const int32_t* top_k;      /* device [batch] or NULL; <= 0 or >= vocab: off */
+  const float* top_p;        /* device [batch] or NULL; >= 1 or NaN: off */
+  const float* min_p;        /* device [batch] or NULL; <= 0 or NaN: off; above 1 counts as 1 */
+  int32_t* token;            /* device [batch] */
+  float* logprob;            /* device [batch] or NULL: log of the token's share of the kept weights (greedy rows: 0) */
+  void* workspace;           /* device, 256-byte aligned: harli_sample_workspace_bytes(batch, vocab); calls that overlap need their own */
+  size_t workspace_bytes;
+} harli_sample_batch;
+harli_status harli_sample(const harli_sample_batch* b, void* hip_stream);
+size_t harli_sample_workspace_bytes(int32_t batch, int32_t vocab);
+
+/* ======================================================================== *
  * Finetune unit (Sec. 6.1): one transformer layer x one micro-batch.
  * ======================================================================== */
 typedef struct harli_saved harli_saved;

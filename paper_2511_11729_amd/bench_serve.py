@@ -10,6 +10,9 @@ it.  Prints one JSON line: time per output token (p50 / p99 / max, share of step
 finetune tokens/s, admission stalls, pre-emptions, finetune out-of-memory retries and the pool's chunk census over
 time.  --pool-gb sizes the slab: roomy by default, tight to exercise the coordination.
 
+--temperature (with --top-k, --top-p, --min-p) draws the tokens instead of taking the most likely ones.  --kv-budget N
+keeps every sequence's cache inside N tokens: the least attended ones leave and their pages go back to the pool.
+
 --sched profiles the latency predictor on compute-unit partitions first (Sec. 5: Eq. 1 per level on the whole model,
 Eq. 2 beside whole training steps) and then lets the runtime scheduler (Sec. 6.2) place both tasks at the beginning of
 every decode phase: decode on the first tenths of the compute units, the finetune task's next layer unit on the last
@@ -292,6 +295,12 @@ def main():
     ap.add_argument("--no-feedback", action="store_true",
                     help="with --sched: plan with the profiled predictor alone, without folding measured step times back in")
     ap.add_argument("--dump", default=None, help="with --sched: per-step records (batch, plan, predicted and measured times) as CSV")
+    ap.add_argument("--temperature", type=float, default=None, help="draw tokens at this temperature (default: the most likely token)")
+    ap.add_argument("--top-k", type=int, default=0)
+    ap.add_argument("--top-p", type=float, default=1.0)
+    ap.add_argument("--min-p", type=float, default=0.0)
+    ap.add_argument("--kv-budget", type=int, default=None, metavar="TOKENS",
+                    help="cached tokens per sequence: past it the least attended ones leave, a page's worth at a time")
     ap.add_argument("--sched-margin", type=float, default=0.9, help="the scheduler plans for this fraction of the target")
     args = ap.parse_args()
 
@@ -309,7 +318,10 @@ def main():
     with torch.cuda.stream(sD):
         keep[-1].zero_()                             # first use of the stream now (its hardware queue is set up here)
     sD.synchronize()
-    server = serve.DecodeServer(ctx, pool, m, max_batch=args.max_batch, max_len=args.max_len, stream=sD, slab=keep[0])
+    sampling = None if args.temperature is None else serve.Sampling(args.temperature, args.top_k, args.top_p, args.min_p)
+    budget = None if args.kv_budget is None else serve.KvBudget(args.kv_budget)
+    server = serve.DecodeServer(ctx, pool, m, max_batch=args.max_batch, max_len=args.max_len, stream=sD, slab=keep[0], sampling=sampling,
+                                budget=budget)
     arrivals = wl.make_arrivals(w, args.steps, tuple(args.targets), args.mean_out,
                                 prompt=w.decode.len_dist if w.decode.len_dist[0] == "lognormal" else ("lognormal", 800, 0.6, 8192))
     arrivals = [[(min(p, args.max_len - 2), o) for p, o in reqs] for reqs in arrivals]

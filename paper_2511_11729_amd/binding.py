@@ -82,6 +82,32 @@ class DecodeBatch(C.Structure):
                 ("max_pages", C.c_int32), ("max_kv_len", C.c_int32)]
 
 
+class Tracking(C.Structure):
+    _fields_ = [("records", C.c_void_p), ("decay", C.c_float), ("position", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class AttendBatch(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("layer", C.c_int32), ("q", C.c_void_p), ("out", C.c_void_p), ("n_tokens", C.c_void_p),
+                ("page_table", C.c_void_p), ("max_pages", C.c_int32), ("max_kv_len", C.c_int32), ("track", Tracking)]
+
+
+class RecordBatch(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n_tokens", C.c_void_p), ("page_table", C.c_void_p), ("max_pages", C.c_int32),
+                ("max_kv_len", C.c_int32), ("records", C.c_void_p)]
+
+
+class EvictBatch(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n_tokens", C.c_void_p), ("keep", C.c_void_p), ("position", C.c_void_p), ("page_table", C.c_void_p),
+                ("max_pages", C.c_int32), ("max_kv_len", C.c_int32), ("sink", C.c_int32), ("recent", C.c_int32),
+                ("records", C.c_void_p), ("n_left", C.c_void_p)]
+
+
+class SampleBatch(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("vocab", C.c_int32), ("logits", C.c_void_p), ("ld", C.c_int64), ("uniform", C.c_void_p),
+                ("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p),
+                ("token", C.c_void_p), ("logprob", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
 _lib = None
 
 _SIGS = {
@@ -104,6 +130,13 @@ _SIGS = {
     "harli_decode_step": (C.c_int, [C.c_void_p, C.POINTER(DecodeBatch), C.c_void_p]),
     "harli_decode_step_static": (C.c_int, [C.c_void_p, C.POINTER(DecodeBatch), C.c_void_p]),
     "harli_decode_step_static_bytes": (C.c_size_t, [C.c_void_p, C.c_int32, C.c_int32]),
+    "harli_decode_step_tracked": (C.c_int, [C.c_void_p, C.POINTER(DecodeBatch), C.POINTER(Tracking), C.c_void_p]),
+    "harli_kv_attend": (C.c_int, [C.c_void_p, C.POINTER(AttendBatch), C.c_void_p]),
+    "harli_kv_attend_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_int32, C.c_int32]),
+    "harli_kv_record_init": (C.c_int, [C.c_void_p, C.POINTER(RecordBatch), C.c_void_p]),
+    "harli_kv_evict": (C.c_int, [C.c_void_p, C.POINTER(EvictBatch), C.c_void_p]),
+    "harli_sample": (C.c_int, [C.POINTER(SampleBatch), C.c_void_p]),
+    "harli_sample_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32]),
     "harli_lora_fwd": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
                                  C.POINTER(C.c_void_p), C.c_void_p]),
     "harli_lora_bwd": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
@@ -371,6 +404,41 @@ class Context:
     def decode_step_static_bytes(self, batch: int, max_kv_len: int) -> int:
         return int(lib().harli_decode_step_static_bytes(self.handle, batch, max_kv_len))
 
+    # ---- a cache inside a budget (harli_kv_*).  track: device records [n_layers, page ids, n_kv_heads, page_tokens, 2], four bytes each:
+    # the weight as fp32 bits, the position as int32
+    def decode_step_tracked(self, *, batch, kv_len, page_table, max_pages, max_kv_len, track, workspace, decay=1.0, position=None,
+                            token_ids=None, x_in=None, x_out=None, logits=None, next_token=None, stream=None) -> None:
+        b = DecodeBatch(batch, _ptr(token_ids), _ptr(x_in), _ptr(x_out), _ptr(logits), _ptr(next_token), _ptr(kv_len),
+                        _ptr(page_table), max_pages, max_kv_len)
+        t = self._tracking(track, decay, position, workspace)
+        _check(lib().harli_decode_step_tracked(self.handle, C.byref(b), C.byref(t), _stream(stream)))
+
+    def kv_attend(self, *, layer, batch, q, out, n_tokens, page_table, max_pages, max_kv_len, workspace, track=None, decay=1.0,
+                  position=None, stream=None) -> None:
+        """Attention of one new token per sequence over one layer's cache; with `track`, the weight of every cached token."""
+        b = AttendBatch(batch, layer, _ptr(q), _ptr(out), _ptr(n_tokens), _ptr(page_table), max_pages, max_kv_len,
+                        self._tracking(track, decay, position, workspace))
+        _check(lib().harli_kv_attend(self.handle, C.byref(b), _stream(stream)))
+
+    def kv_attend_workspace_bytes(self, batch: int, max_kv_len: int) -> int:
+        return int(lib().harli_kv_attend_workspace_bytes(self.handle, batch, max_kv_len))
+
+    def kv_record_init(self, *, batch, n_tokens, page_table, max_pages, max_kv_len, track, stream=None) -> None:
+        """Records of a prompt's tokens: weight 0, position their index."""
+        b = RecordBatch(batch, _ptr(n_tokens), _ptr(page_table), max_pages, max_kv_len, _ptr(track))
+        _check(lib().harli_kv_record_init(self.handle, C.byref(b), _stream(stream)))
+
+    def kv_evict(self, *, batch, n_tokens, keep, page_table, max_pages, max_kv_len, track, sink=0, recent=0, position=None, n_left=None,
+                 stream=None) -> None:
+        """Every layer and KV head of sequence b keeps its best keep[b] tokens, in its first keep[b] slots."""
+        b = EvictBatch(batch, _ptr(n_tokens), _ptr(keep), _ptr(position), _ptr(page_table), max_pages, max_kv_len, sink, recent,
+                       _ptr(track), _ptr(n_left))
+        _check(lib().harli_kv_evict(self.handle, C.byref(b), _stream(stream)))
+
+    @staticmethod
+    def _tracking(track, decay, position, workspace) -> Tracking:
+        return Tracking(_ptr(track), decay, _ptr(position), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
+
     def lora_fwd(self, layer: int, X, Y, B_f: int, S: int, stream=None) -> int:
         saved = C.c_void_p()
         _check(lib().harli_lora_fwd(self.handle, layer, _ptr(X), _ptr(Y), B_f, S, C.byref(saved), _stream(stream)))
@@ -406,6 +474,18 @@ def adamw_step(master, m, v, grad, param_bf16, *, step: int, lr=1e-3, beta1=0.9,
     cfg = AdamWCfg(lr, beta1, beta2, eps, weight_decay, grad_scale, step, int(zero_grad))
     _check(lib().harli_adamw_step(_ptr(master), _ptr(m), _ptr(v), _ptr(grad), _ptr(param_bf16), master.numel(), C.byref(cfg),
                                   _stream(stream)))
+
+
+def sample(logits, uniform, token, *, workspace, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, stream=None) -> None:
+    """A token per row of logits (fp32 [batch, vocab], rows may lie apart) from the random numbers `uniform`; the settings are device
+    tensors [batch] or None.  workspace: sample_workspace_bytes(batch, vocab) bytes on the device."""
+    b = SampleBatch(logits.shape[0], logits.shape[1], _ptr(logits), logits.stride(0), _ptr(uniform), _ptr(temperature), _ptr(top_k),
+                    _ptr(top_p), _ptr(min_p), _ptr(token), _ptr(logprob), _ptr(workspace), workspace.numel() * workspace.element_size())
+    _check(lib().harli_sample(C.byref(b), _stream(stream)))
+
+
+def sample_workspace_bytes(batch: int, vocab: int) -> int:
+    return int(lib().harli_sample_workspace_bytes(batch, vocab))
 
 
 # ----------------------------------------------------------------------------- predictor / scheduler (harli_sched.h)

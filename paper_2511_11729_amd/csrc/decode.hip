@@ -37,6 +37,7 @@
 #include <algorithm>
 #include <mutex>
 
+#include "attend.h"
 #include "ctx.h"
 #include "decode_large.h"
 #include "device_utils.h"
@@ -387,7 +388,7 @@ struct AttnList {
 __global__ void __launch_bounds__(256) k_decode_prep(int H, int d, int n_ssq, int bpad, int ssq_np, const int* token_ids,
                                                      const unsigned short* emb, int vocab, const float* x_in, float* xa,
                                                      const float* g1, unsigned short* hx1, float* ssq, float* rope,
-                                                     const int* kv_len, const double* inv_freq, int* err_flag, AttnList list) {
+                                                     const int* kv_len, const int* position, const double* inv_freq, int* err_flag, AttnList list) {
   const int b = blockIdx.x, tid = threadIdx.x;
   const int steps = (H + 31) >> 5;
   float s2 = 0.f;
@@ -444,7 +445,7 @@ __global__ void __launch_bounds__(256) k_decode_prep(int H, int d, int n_ssq, in
     for (int i = tid; i < mine; i += 256) list.item[first + i] = b << 16 | i;
     if (b == (int)gridDim.x - 1 && tid == 0) *list.total = first + mine;
   }
-  const double pos = (double)kv_len[b];
+  const double pos = (double)(position ? position[b] : kv_len[b]);
   for (int i = tid; i < half; i += 256) {
     // angle = pos * base^(-2i/d) in double, reduced to [-pi, pi] before the fp32 sin/cos
     const double ang = pos * inv_freq[i];
@@ -505,18 +506,22 @@ __device__ __forceinline__ bool attn_place(const AttnList& list, int n_kv, int& 
   return true;
 }
 
-template <int D, int G, int CH, bool CACHED, bool LIST>
+//
+// ATT: the form behind harli_kv_attend and tracked steps.  Every chunk writes its partial (apart: (max, sum) pairs and rows), and
+// the scores go out as they are, in the log2 domain, for k_attend_finish to make weights of once maximum and sum are known.  The
+// lanes of a token hold its score alike: lane dg keeps that of the wave's dg-th group of tokens, so that one store takes them all.
+template <int D, int G, int CH, bool CACHED, bool LIST, bool ATT>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(attn_min_waves<D, G>(), 8))) k_paged_attn(const float* qbuf, const int* kv_len, const int* page_table,
                                                     int max_pages, int layer, int n_q, int n_kv, const char* slab,
                                                     KvGeom geom, float* part, int max_chunks, unsigned short* obuf,
-                                                    int* err_flag, AttnList list) {
+                                                    int* err_flag, AttnList list, AttendWs att) {
   constexpr int LPT = D / 8;         // lanes per token
   constexpr int TPI = 64 / LPT;      // tokens per load instruction
   constexpr int IT = kPageTokens / TPI;
   constexpr int PW = CH / kPageTokens / 4;  // pages per wave
   int b, c, ch;
   if (!attn_place<LIST>(list, n_kv, b, c, ch)) return;
-  const int n_tot = kv_len[b] + 1;
+  const int n_tot = kv_len[b] + (ATT ? att.n_new : 1);
   // the grid covers the caller's bound max_kv_len: a longer sequence would lose its newest tokens without a word
   if (ch == 0 && c == 0 && threadIdx.x == 0 && (n_tot > list.n_chunks * CH || n_tot > max_pages * kPageTokens))
     atomicOr(err_flag, 4);
@@ -596,6 +601,19 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(attn_m
         mw[gq] = fmaxf(mw[gq], s);
       }
     }
+  if constexpr (ATT) {
+    if (att.scores) {
+      static_assert(PW * IT <= LPT, "a lane of a token for every group of tokens of the wave");
+#pragma unroll
+      for (int gq = 0; gq < G; ++gq) {
+        float s = sc[gq][0][0];
+#pragma unroll
+        for (int i = 1; i < PW * IT; ++i) s = dg == i ? sc[gq][i / IT][i % IT] : s;
+        if (dg < PW * IT)
+          att.scores[((size_t)b * n_q + c * G + gq) * att.score_ld + ch * CH + (wave * PW + dg / IT) * kPageTokens + dg % IT * TPI + tl] = s;
+      }
+    }
+  }
   float lw[G], acc[G][8];
 #pragma unroll
   for (int gq = 0; gq < G; ++gq) {
@@ -656,7 +674,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(attn_m
       o += s_o[w][gq][e] * f;
     }
     const int head = c * G + gq;
-    if (list.n_chunks == 1) {
+    if constexpr (ATT) {
+      const size_t at = ((size_t)b * n_q + head) * list.n_chunks + ch;
+      att.o[at * D + e] = o;
+      if (e == 0) *reinterpret_cast<float2*>(att.ml + at * 2) = make_float2(M, L);
+    } else if (list.n_chunks == 1) {
       obuf[xfrag_off(b, head * D + e, steps_o)] = f2bf(o / L);
     } else {
       float* p = part + (((size_t)b * n_q + head) * max_chunks + ch) * (D + 2);
@@ -706,17 +728,17 @@ __device__ __forceinline__ bf16x8 transposed_8(char* p0, char* p1) {
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-template <int G, int CH, bool LIST>
+template <int G, int CH, bool LIST, bool ATT>
 __global__ void __launch_bounds__(256) k_paged_attn_mm(const float* qbuf, const int* kv_len, const int* page_table, int max_pages,
                                                        int layer, int n_q, int n_kv, const char* slab, KvGeom geom, float* part,
-                                                       int max_chunks, unsigned short* obuf, int* err_flag, AttnList list) {
+                                                       int max_chunks, unsigned short* obuf, int* err_flag, AttnList list, AttendWs att) {
   constexpr int D = 128, PW = CH / kPageTokens / 4, QG = 8, NT = 2;  // queries per term, products per step
   static_assert(G <= QG && PW % 2 == 0 && G * D * 4 <= PW * 4096, "whole steps of 32 tokens; a wave's output fits its share of V");
   __shared__ __align__(1024) char s_v[4 * PW * 4096];
   __shared__ float s_m[4][G], s_l[4][G];
   int b, c, ch;
   if (!attn_place<LIST>(list, n_kv, b, c, ch)) return;
-  const int n_tot = kv_len[b] + 1;
+  const int n_tot = kv_len[b] + (ATT ? att.n_new : 1);
   // the grid covers the caller's bound max_kv_len: a longer sequence would lose its newest tokens without a word
   if (ch == 0 && c == 0 && threadIdx.x == 0 && (n_tot > list.n_chunks * CH || n_tot > max_pages * kPageTokens))
     atomicOr(err_flag, 4);
@@ -800,6 +822,11 @@ __global__ void __launch_bounds__(256) k_paged_attn_mm(const float* qbuf, const 
       sc[pp][e] = v;
       m = fmaxf(m, v);
     }
+    if constexpr (ATT) {  // a lane has four tokens in a row of query i16
+      if (att.scores && i16 < G)
+        *reinterpret_cast<float4*>(att.scores + ((size_t)b * n_q + c * G + i16) * att.score_ld + ch * CH + (wave * PW + pp) * kPageTokens + 4 * g) =
+            make_float4(sc[pp][0], sc[pp][1], sc[pp][2], sc[pp][3]);
+    }
   }
   m = fmaxf(m, __shfl_xor(m, 16, 64));
   m = fmaxf(m, __shfl_xor(m, 32, 64));
@@ -865,7 +892,11 @@ __global__ void __launch_bounds__(256) k_paged_attn_mm(const float* qbuf, const 
       acc += reinterpret_cast<const float*>(s_v + w * (PW * 4096))[idx] * f;
     }
     const int head = c * G + gq;
-    if (list.n_chunks == 1) {
+    if constexpr (ATT) {
+      const size_t at = ((size_t)b * n_q + head) * list.n_chunks + ch;
+      att.o[at * D + e] = acc;
+      if (e == 0) *reinterpret_cast<float2*>(att.ml + at * 2) = make_float2(M, L);
+    } else if (list.n_chunks == 1) {
       obuf[xfrag_off(b, head * D + e, steps_o)] = f2bf(acc / L);
     } else {
       float* p = part + (((size_t)b * n_q + head) * max_chunks + ch) * (D + 2);
@@ -1066,6 +1097,19 @@ void dispatch_skinny(SkinnyArgs a, int n_tiles, hipStream_t st) {
   }
 }
 
+// What stays in the memory-side cache from step to step (step_stream_bytes has the figures).
+constexpr size_t kMemorySideCache = (size_t)256 << 20;
+
+// What an attention launch reads and writes, beside the context's own.
+struct AttnArgs {
+  const float* q;  // [batch][n_q][d]
+  const int *kv_len, *page_table;
+  int batch, max_pages, layer;
+  float* part;     // partials of the untracked form, and their row length
+  int max_chunks;
+  unsigned short* obuf;
+};
+
 // tokens per attention chunk, as decode_step_bf16 launches them
 constexpr int attn_chunk(int d, int G) { return d == 64 || G <= 2 ? 256 : 128; }
 // Workgroups of the attention grid from which it follows a list.  What the list is worth follows the share of them that hold tokens,
@@ -1076,34 +1120,63 @@ constexpr int attn_chunk(int d, int G) { return d == 64 || G <= 2 ? 256 : 128; }
 // on the gain at uneven lengths is the larger.  (Reading the number of chunks and the item in one trip changes none of this.)
 constexpr int kListedWorkgroups = 4096;
 
-template <int D, int G, int CH>
-void launch_attn(harli_ctx* c, const DecodeWs& w, const harli_decode_batch* b, int layer, bool cached, AttnList list, hipStream_t st) {
+template <int D, int G, int CH, bool ATT>
+void launch_attn(harli_ctx* c, const AttnArgs& a, bool cached, AttnList list, const AttendWs& att, hipStream_t st) {
   const harli_model_cfg& m = c->cfg;
   static_assert(CH == attn_chunk(D, G), "the list counts these chunks");
   const int n_chunks = list.n_chunks;
 #define ATTN_LAUNCH(kernel)                                                                                             \
-  hipLaunchKernelGGL(kernel, list.item ? dim3(n_chunks * m.n_kv_heads * b->batch) : dim3(n_chunks, m.n_kv_heads, b->batch), dim3(256), 0, st, w.qbuf, b->kv_len, b->page_table, \
-                     b->max_pages, layer, m.n_q_heads, m.n_kv_heads, c->slab, c->geom, w.att_part, w.max_chunks,         \
-                     static_cast<unsigned short*>(w.obuf), w.err_flag, list)
+  hipLaunchKernelGGL(kernel, list.item ? dim3(n_chunks * m.n_kv_heads * a.batch) : dim3(n_chunks, m.n_kv_heads, a.batch), dim3(256), 0, st, a.q, a.kv_len, a.page_table, \
+                     a.max_pages, a.layer, m.n_q_heads, m.n_kv_heads, c->slab, c->geom, a.part, a.max_chunks, a.obuf, c->dw.err_flag, list, att)
   if constexpr (D == 128 && G >= 5) {
-    if (list.item) ATTN_LAUNCH((k_paged_attn_mm<G, CH, true>));
-    else ATTN_LAUNCH((k_paged_attn_mm<G, CH, false>));
+    if (list.item) ATTN_LAUNCH((k_paged_attn_mm<G, CH, true, ATT>));
+    else ATTN_LAUNCH((k_paged_attn_mm<G, CH, false, ATT>));
   } else {
-    if (cached) ATTN_LAUNCH((k_paged_attn<D, G, CH, true, false>));
-    else if (list.item) ATTN_LAUNCH((k_paged_attn<D, G, CH, false, true>));
-    else ATTN_LAUNCH((k_paged_attn<D, G, CH, false, false>));
+    if (cached) ATTN_LAUNCH((k_paged_attn<D, G, CH, true, false, ATT>));
+    else if (list.item) ATTN_LAUNCH((k_paged_attn<D, G, CH, false, true, ATT>));
+    else ATTN_LAUNCH((k_paged_attn<D, G, CH, false, false, ATT>));
   }
 #undef ATTN_LAUNCH
-  if (n_chunks > 1)
-    hipLaunchKernelGGL((k_attn_merge<D, CH>), dim3(m.n_q_heads, b->batch), dim3(D), 0, st, w.att_part, b->kv_len,
-                       m.n_q_heads, w.max_chunks, static_cast<unsigned short*>(w.obuf));
+  if (!ATT && n_chunks > 1)
+    hipLaunchKernelGGL((k_attn_merge<D, CH>), dim3(m.n_q_heads, a.batch), dim3(D), 0, st, a.part, a.kv_len,
+                       m.n_q_heads, a.max_chunks, a.obuf);
+}
+
+template <bool ATT>
+harli_status dispatch_attn(harli_ctx* c, const AttnArgs& a, bool cached, const AttnList& list, const AttendWs& att, hipStream_t st) {
+  const int d = c->cfg.head_dim, G = c->cfg.n_q_heads / c->cfg.n_kv_heads;
+  if (d == 128 && G == 1) launch_attn<128, 1, 256, ATT>(c, a, cached, list, att, st);
+  else if (d == 128 && G == 2) launch_attn<128, 2, 256, ATT>(c, a, cached, list, att, st);
+  else if (d == 128 && G == 4) launch_attn<128, 4, 128, ATT>(c, a, cached, list, att, st);
+  else if (d == 128 && G == 8) launch_attn<128, 8, 128, ATT>(c, a, cached, list, att, st);
+  else if (d == 128 && G == 3) launch_attn<128, 3, 128, ATT>(c, a, cached, list, att, st);
+  else if (d == 128 && G == 5) launch_attn<128, 5, 128, ATT>(c, a, cached, list, att, st);
+  else if (d == 128 && G == 6) launch_attn<128, 6, 128, ATT>(c, a, cached, list, att, st);
+  else if (d == 128 && G == 7) launch_attn<128, 7, 128, ATT>(c, a, cached, list, att, st);
+  else if (d == 64 && G == 1) launch_attn<64, 1, 256, ATT>(c, a, cached, list, att, st);
+  else if (d == 64 && G == 2) launch_attn<64, 2, 256, ATT>(c, a, cached, list, att, st);
+  else if (d == 64 && G == 4) launch_attn<64, 4, 256, ATT>(c, a, cached, list, att, st);
+  else return fail(HARLI_ERR_INVALID, "decode_step: head_dim %d with group %d is not supported", d, G);
+  return HARLI_OK;
 }
 
 }  // namespace
 
 namespace harli {
 
-harli_status decode_step_f32(harli_ctx* c, const harli_decode_batch* b, hipStream_t st);  // decode_generic.hip
+int attend_chunk_bf16(int d, int G) { return attn_chunk(d, G); }
+
+// The chunks of harli_kv_attend on bf16 storage (k_attend_finish joins them).
+harli_status attend_bf16(harli_ctx* c, const harli_attend_batch* b, const AttendWs& att, hipStream_t st) {
+  AttnList list{};
+  list.chunk = att.chunk;
+  list.n_chunks = att.n_chunks;
+  const size_t kv = (size_t)b->batch * b->max_kv_len * c->cfg.n_kv_heads * c->cfg.head_dim * 4;  // keys and values, two bytes each
+  const AttnArgs a{b->q, b->n_tokens, b->page_table, b->batch, b->max_pages, b->layer, nullptr, 0, nullptr};
+  return dispatch_attn<true>(c, a, kv <= kMemorySideCache, list, att, st);
+}
+
+harli_status decode_step_f32(harli_ctx* c, const harli_decode_batch* b, hipStream_t st, const harli_tracking* tr);  // decode_generic.hip
 
 size_t packed_weight_elems(int N, int K) { return (size_t)((N + 15) / 16) * ((K + 31) / 32) * 512; }
 
@@ -1148,7 +1221,6 @@ harli_status check_decode_args(harli_ctx* c, const harli_decode_batch* b) {
 // memory-side cache is there from the step before, and nontemporal loads would fetch it from memory every time.  A step in us
 // with nontemporal / ordinary loads: 28 MiB (hidden size 512) 118 / 106, 155 MiB (1024) 193 / 176, 199 MiB (1536) 142 / 130,
 // 268 MiB (2048) 130 / 127, 357 MiB 172 / 174, 412 MiB (one 7B layer) 92 / 97.
-constexpr size_t kMemorySideCache = (size_t)256 << 20;
 size_t step_stream_bytes(const harli_ctx* c, const harli_decode_batch* b) {
   const harli_model_cfg& m = c->cfg;
   const size_t QD = (size_t)m.n_q_heads * m.head_dim, KVD = (size_t)m.n_kv_heads * m.head_dim, H = m.hidden;
@@ -1156,7 +1228,8 @@ size_t step_stream_bytes(const harli_ctx* c, const harli_decode_batch* b) {
   return 2 * (m.n_layers * (layer + kv) + (b->logits ? H * m.vocab : 0));
 }
 
-harli_status decode_step_bf16(harli_ctx* c, const harli_decode_batch* b, hipStream_t st, const DecodeWs& w) {
+// `tr`: what a tracked step adds, or null.
+harli_status decode_step_bf16(harli_ctx* c, const harli_decode_batch* b, hipStream_t st, const DecodeWs& w, const harli_tracking* tr) {
   const harli_model_cfg& m = c->cfg;
   const int B = b->batch, H = m.hidden, d = m.head_dim, QD = m.n_q_heads * d, F = m.ffn, L = m.n_layers;
   const int n_ssq = 2 * L + 1;
@@ -1166,11 +1239,12 @@ harli_status decode_step_bf16(harli_ctx* c, const harli_decode_batch* b, hipStre
   AttnList list{};
   list.chunk = attn_chunk(d, G);
   list.n_chunks = (b->max_kv_len + list.chunk - 1) / list.chunk;
+  const AttendWs att = tr ? attend_layout(c, B, b->max_kv_len, tr->workspace, true, 1) : AttendWs{};
   const long long att_wgs = (long long)list.n_chunks * B * m.n_kv_heads;
   if (w.att_list && !cached && att_wgs >= kListedWorkgroups && att_wgs < (1ll << 23) && list.n_chunks < (1 << 16)) list.total = w.att_list, list.item = w.att_list + 16;
   hipLaunchKernelGGL(k_decode_prep, dim3(B), dim3(256), 0, st, H, d, n_ssq, w.bpad, np, b->token_ids,
                      static_cast<const unsigned short*>(c->emb), m.vocab, b->x_in, w.xa, c->layers[0].g1,
-                     static_cast<unsigned short*>(w.hx1), w.ssq, w.rope, b->kv_len, w.inv_freq, w.err_flag, list);
+                     static_cast<unsigned short*>(w.hx1), w.ssq, w.rope, b->kv_len, tr ? tr->position : nullptr, w.inv_freq, w.err_flag, list);
 
   const float* xcur = b->token_ids ? w.xa : b->x_in;
   float* ping[2] = {w.xb, w.xa};  // layer l writes ping[l&1]; layer 0 must not overwrite xa (it can be its input)
@@ -1215,18 +1289,15 @@ harli_status decode_step_bf16(harli_ctx* c, const harli_decode_batch* b, hipStre
       dispatch_skinny<MODE_QKV>(a, (m.n_q_heads + 2 * m.n_kv_heads) * (d / 16), st);
     }
     // --- attention
-    if (d == 128 && G == 1) launch_attn<128, 1, 256>(c, w, b, l, cached, list, st);
-    else if (d == 128 && G == 2) launch_attn<128, 2, 256>(c, w, b, l, cached, list, st);
-    else if (d == 128 && G == 4) launch_attn<128, 4, 128>(c, w, b, l, cached, list, st);
-    else if (d == 128 && G == 8) launch_attn<128, 8, 128>(c, w, b, l, cached, list, st);
-    else if (d == 128 && G == 3) launch_attn<128, 3, 128>(c, w, b, l, cached, list, st);
-    else if (d == 128 && G == 5) launch_attn<128, 5, 128>(c, w, b, l, cached, list, st);
-    else if (d == 128 && G == 6) launch_attn<128, 6, 128>(c, w, b, l, cached, list, st);
-    else if (d == 128 && G == 7) launch_attn<128, 7, 128>(c, w, b, l, cached, list, st);
-    else if (d == 64 && G == 1) launch_attn<64, 1, 256>(c, w, b, l, cached, list, st);
-    else if (d == 64 && G == 2) launch_attn<64, 2, 256>(c, w, b, l, cached, list, st);
-    else if (d == 64 && G == 4) launch_attn<64, 4, 256>(c, w, b, l, cached, list, st);
-    else return fail(HARLI_ERR_INVALID, "decode_step: head_dim %d with group %d is not supported", d, G);
+    const AttnArgs aa{w.qbuf, b->kv_len, b->page_table, B, b->max_pages, l, w.att_part, w.max_chunks, static_cast<unsigned short*>(w.obuf)};
+    if (tr) {
+      const harli_status rc = dispatch_attn<true>(c, aa, cached, list, att, st);
+      if (rc != HARLI_OK) return rc;
+      attend_finish(c, att, b->kv_len, b->page_table, B, b->max_pages, l, nullptr, aa.obuf, tr, st);
+    } else {
+      const harli_status rc = dispatch_attn<false>(c, aa, cached, list, att, st);
+      if (rc != HARLI_OK) return rc;
+    }
     // --- output projection + residual, operand of the FFN
     a.x = static_cast<const unsigned short*>(w.obuf);
     a.K = QD;
@@ -1350,8 +1421,19 @@ extern "C" harli_status harli_decode_step(harli_ctx* c, const harli_decode_batch
   harli_status s = check_decode_args(c, b);
   if (s != HARLI_OK) return s;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  if (c->cfg.dtype == HARLI_F32) return decode_step_f32(c, b, st);
-  return decode_step_bf16(c, b, st, c->dw);
+  if (c->cfg.dtype == HARLI_F32) return decode_step_f32(c, b, st, nullptr);
+  return decode_step_bf16(c, b, st, c->dw, nullptr);
+}
+
+extern "C" harli_status harli_decode_step_tracked(harli_ctx* c, const harli_decode_batch* b, const harli_tracking* t, void* hip_stream) {
+  harli_status s = check_decode_args(c, b);
+  if (s != HARLI_OK) return s;
+  if (!t || !t->records) return fail(HARLI_ERR_INVALID, "decode_step_tracked: records are required");
+  s = check_tracking(c, t, b->batch, b->max_kv_len, "decode_step_tracked");
+  if (s != HARLI_OK) return s;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (c->cfg.dtype == HARLI_F32) return decode_step_f32(c, b, st, t);
+  return decode_step_bf16(c, b, st, c->dw, t);
 }
 
 extern "C" int32_t harli_decode_tiled_min_batch(void) { return dg_min_batch(); }
@@ -1421,5 +1503,5 @@ extern "C" harli_status harli_decode_step_static(harli_ctx* c, const harli_decod
   // producers and their padding by the step's first kernel; batch rows past `batch` only reach output columns that are never stored).
   const size_t n16 = operand_bytes / 16;
   hipLaunchKernelGGL(k_zero16, dim3((unsigned)((n16 + 255) / 256)), dim3(256), 0, st, reinterpret_cast<uint4*>(base), n16);
-  return decode_step_bf16(c, b, st, w);
+  return decode_step_bf16(c, b, st, w, nullptr);
 }

@@ -6,6 +6,7 @@
 // costs: hidden size 256, four sequences of about 100 tokens took 106 us in fourteen launches and take 21 in five.
 #include <type_traits>
 
+#include "attend.h"
 #include "ctx.h"
 #include "device_utils.h"
 
@@ -163,7 +164,7 @@ __global__ void __launch_bounds__(256) g_gate_up(GLinear p) {
 
 struct GRope {
   const float *bq, *bk, *bv;
-  const int *kv_len, *page_table;
+  const int *kv_len, *page_table, *position;  // position: of the rotation, or null: kv_len
   int max_pages, layer, n_q, n_kv, d;
   const double* inv_freq;
   char* slab;
@@ -171,8 +172,8 @@ struct GRope {
   int* err_flag;
 };
 
-// q, k, v: a wave computes rows i and i + d/2 of one head (a rotary pair; of v, just two rows).  q and k are rotated at position
-// kv_len[b] -- angle pos * base^(-2i/d) evaluated in double -- and k and v appended to the page of that position.
+// q, k, v: a wave computes rows i and i + d/2 of one head (a rotary pair; of v, just two rows).  q and k are rotated at the token's
+// position -- angle pos * base^(-2i/d) evaluated in double -- and k and v appended to the page of that position.
 template <int BT, bool VEC>
 __global__ void __launch_bounds__(256) g_qkv(GLinear p, GRope r) {
   const int lane = threadIdx.x & 63, half = r.d / 2, b0 = blockIdx.y * BT;
@@ -198,7 +199,7 @@ __global__ void __launch_bounds__(256) g_qkv(GLinear p, GRope r) {
     const int pos = r.kv_len[b];
     if (kind < 2) {
       double sn, cs;
-      sincos((double)pos * r.inv_freq[i], &sn, &cs);
+      sincos((double)(r.position ? r.position[b] : pos) * r.inv_freq[i], &sn, &cs);
       const float t = a;
       a = t * (float)cs - c * (float)sn;
       c = c * (float)cs + t * (float)sn;
@@ -372,7 +373,7 @@ void linear(const float* x, const float* g, float eps, const void* W, const floa
 
 }  // namespace
 
-harli_status decode_step_f32(harli_ctx* c, const harli_decode_batch* b, hipStream_t st) {
+harli_status decode_step_f32(harli_ctx* c, const harli_decode_batch* b, hipStream_t st, const harli_tracking* tr) {
   const harli_model_cfg& m = c->cfg;
   DecodeWs& w = c->dw;
   const int B = b->batch, H = m.hidden, d = m.head_dim, QD = m.n_q_heads * d, F = m.ffn, L = m.n_layers;
@@ -382,6 +383,7 @@ harli_status decode_step_f32(harli_ctx* c, const harli_decode_batch* b, hipStrea
   float* q = w.qbuf;
   const float* x = b->x_in;
   float* xn = w.xb;
+  const AttendWs att = tr ? attend_layout(c, B, b->max_kv_len, tr->workspace, true, 1) : AttendWs{};
   if (b->token_ids) {
     hipLaunchKernelGGL(g_input, dim3(B), dim3(256), 0, st, H, b->token_ids, static_cast<const float*>(c->emb), m.vocab, w.xa, w.err_flag);
     x = w.xa;
@@ -391,7 +393,7 @@ harli_status decode_step_f32(harli_ctx* c, const harli_decode_batch* b, hipStrea
     {
       const GLinear p{x, lw.g1, {static_cast<const float*>(lw.w[0]), static_cast<const float*>(lw.w[1]), static_cast<const float*>(lw.w[2])},
                       nullptr, q, B, H, QD, m.rms_eps};
-      const GRope r{lw.bias[0], lw.bias[1], lw.bias[2], b->kv_len, b->page_table, b->max_pages, l, m.n_q_heads, m.n_kv_heads, d, w.inv_freq,
+      const GRope r{lw.bias[0], lw.bias[1], lw.bias[2], b->kv_len, b->page_table, tr ? tr->position : nullptr, b->max_pages, l, m.n_q_heads, m.n_kv_heads, d, w.inv_freq,
                     c->slab, c->geom, w.err_flag};
       pick(p, 3, [&](auto bt, auto v4) {
         constexpr int BT = decltype(bt)::value;
@@ -401,7 +403,10 @@ harli_status decode_step_f32(harli_ctx* c, const harli_decode_batch* b, hipStrea
 #define G_ATT(EL_)                                                                                                     \
   hipLaunchKernelGGL(g_attention<EL_>, dim3(m.n_q_heads, B, (d + 64 * EL_ - 1) / (64 * EL_)), dim3(256), 0, st, q, b->kv_len, b->page_table, b->max_pages, l, \
                      m.n_q_heads, m.n_kv_heads, d, c->slab, c->geom, m.max_seq_len, o, w.err_flag)
-    if (d <= 64) G_ATT(1);
+    if (tr) {
+      attend_f32(c, q, b->kv_len, b->page_table, B, b->max_pages, l, att, st);
+      attend_finish(c, att, b->kv_len, b->page_table, B, b->max_pages, l, o, nullptr, tr, st);
+    } else if (d <= 64) G_ATT(1);
     else if (d <= 128) G_ATT(2);
     else if (d <= 256) G_ATT(4);
     else G_ATT(16);

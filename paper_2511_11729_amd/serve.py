@@ -8,10 +8,16 @@ prompt's KV pages from the pool; every decode step appends one token per running
 sequence crosses a page boundary and frees the pages of sequences that finish (the pool reuses them once the step
 that last read them has completed).  The finetune task allocates its saved activations from the same pool and backs
 off when the pool reports pressure or cannot serve it (Sec. 4.4: inference has priority).
+
+Two options: `Sampling` draws the tokens instead of taking the most likely ones, and `KvBudget` keeps every sequence's
+cache inside a number of tokens -- steps add up the attention weight each cached token receives, and when a sequence has
+grown past the budget its least attended tokens leave, in every layer and KV head by its own choice, and the pages
+behind the kept length go back to the pool.
 """
 from __future__ import annotations
 
 import collections
+import dataclasses
 import threading
 import time
 
@@ -23,10 +29,32 @@ from . import binding as hb
 P = 16  # tokens per KV page
 
 
+@dataclasses.dataclass(frozen=True)
+class Sampling:
+    """How tokens are drawn (harli_sample); the random numbers come from a generator on the device, seeded here."""
+    temperature: float = 1.0
+    top_k: int = 0
+    top_p: float = 1.0
+    min_p: float = 0.0
+    seed: int = 0
+
+
+@dataclasses.dataclass(frozen=True)
+class KvBudget:
+    """A sequence that holds `keep` + `slack` tokens is cut to `keep` (harli_kv_evict): the first `sink` and the last `recent`
+    positions stay, of the others those with the most accumulated attention weight."""
+    keep: int
+    slack: int = P
+    sink: int = 4
+    recent: int = 64
+    decay: float = 1.0
+
+
 class DecodeServer:
     """Continuous batching over `harli_decode_step`.  Not thread-safe: one thread drives it."""
 
-    def __init__(self, ctx, pool, m, *, max_batch: int, max_len: int, stream, slab=None):
+    def __init__(self, ctx, pool, m, *, max_batch: int, max_len: int, stream, slab=None, sampling: Sampling | None = None,
+                 budget: KvBudget | None = None):
         """slab: the pool's slab as a torch uint8 tensor; when given, the KV pages of an admitted prompt are cleared on
         the decode stream (standing in for the arrival of the prompt's cache from the prefill instance: the same
         bytes are written once).  Without it the pages keep whatever the pool last held there."""
@@ -59,7 +87,29 @@ class DecodeServer:
         self.nxt = torch.zeros(max_batch, dtype=torch.int32, device=dev)
         self.logits = torch.empty(max_batch, m.vocab, dtype=torch.float32, device=dev)
         self.x_out = torch.empty(max_batch, m.hidden, dtype=torch.float32, device=dev)
-        self.running = []          # per slot: [pages (list), cached tokens, tokens left]
+        self.sampling, self.budget = sampling, budget
+        if sampling is not None:
+            self.gen = torch.Generator(dev).manual_seed(sampling.seed)
+            self.uniform = torch.empty(max_batch, device=dev)
+            full = lambda v, t: torch.full((max_batch,), v, dtype=t, device=dev)  # noqa: E731
+            self.settings = dict(temperature=full(sampling.temperature, torch.float32), top_k=full(sampling.top_k, torch.int32),
+                                 top_p=full(sampling.top_p, torch.float32), min_p=full(sampling.min_p, torch.float32))
+            self.sample_ws = torch.empty(hb.sample_workspace_bytes(max_batch, m.vocab), dtype=torch.uint8, device=dev)
+        if budget is not None:
+            if budget.keep < 1 or budget.slack < 1:
+                raise ValueError("a budget keeps at least one token and cuts at least one")
+            st = pool.stats()
+            self.track = torch.zeros(pool.cfg.n_layers, st.n_chunks * st.pages_per_block, m.n_kv, P, 2, dtype=torch.int32, device=dev)
+            self.attend_ws = torch.empty(ctx.kv_attend_workspace_bytes(max_batch, max_len), dtype=torch.uint8, device=dev)
+            # per step and slot: position of the new token, tokens of a prompt that has just arrived, tokens after the step,
+            # tokens to keep, position of the token after it
+            self.marks = np.zeros((5, max_batch), np.int32)
+            self.marks_ring = [torch.empty(5, max_batch, dtype=torch.int32, pin_memory=True) for _ in self.ring]
+            self.marks_dev = torch.zeros(5, max_batch, dtype=torch.int32, device=dev)
+        if sampling is not None or budget is not None:
+            torch.cuda.current_stream().synchronize()   # the buffers are filled before another stream reads them
+        self.evicted = 0           # tokens (of every layer and KV head alike) that have left the cache under a budget
+        self.running = []          # per slot: [pages (list), cached tokens, tokens left, tokens it has had, just arrived, cut after this step]
         self.queue = collections.deque()
         self.step_no = 0
         self.last_done = None
@@ -119,7 +169,7 @@ class DecodeServer:
             self.table[b, :] = -1
             self.table[b, :need] = ids
             self.kv[b] = prompt
-            self.running.append([list(ids), prompt, out])
+            self.running.append([list(ids), prompt, out, prompt, True, False])
             self.admitted += 1
 
     def _drop(self, b, event):
@@ -147,19 +197,26 @@ class DecodeServer:
             ev.synchronize()                   # the copy that last used this staging buffer is done
         tb[:B].copy_(torch.from_numpy(self.table[:B]))
         kb[:B].copy_(torch.from_numpy(self.kv[:B]))
+        if self.budget is not None:
+            for b, seq in enumerate(self.running):
+                after = seq[1] + 1
+                seq[5] = seq[2] > 1 and after >= self.budget.keep + self.budget.slack   # (not for a sequence that ends with this step)
+                self.marks[:, b] = seq[3], seq[1] if seq[4] else 0, after, self.budget.keep if seq[5] else after, seq[3] + 1
+            marks = self.marks_ring[self.step_no % len(self.ring)]
+            marks.copy_(torch.from_numpy(self.marks))
         if self.last_done is not None:
             self.upload.wait_event(self.last_done)   # the previous step still reads the device copies
         with torch.cuda.stream(self.upload):
             self.table_dev[:B].copy_(tb[:B], non_blocking=True)
             self.kv_dev[:B].copy_(kb[:B], non_blocking=True)
+            if self.budget is not None:
+                self.marks_dev.copy_(marks, non_blocking=True)
             up = torch.cuda.Event()
             up.record()
         self.stream.wait_event(up)
         start = torch.cuda.Event(enable_timing=True)
         start.record(self.stream)
-        max_kv = int(self.kv[:B].max()) + 1
-        self.ctx.decode_step(batch=B, kv_len=self.kv_dev, page_table=self.table_dev, max_pages=self.max_pages, max_kv_len=max_kv,
-                             token_ids=self.tok, x_out=self.x_out, logits=self.logits, next_token=self.nxt, stream=self.stream)
+        self._launch(B, int(self.kv[:B].max()) + 1)
         done = torch.cuda.Event(enable_timing=True)
         done.record(self.stream)
         self._timed.append((start if self.last_done is None or self._idle else self.last_done, done, self.tag))
@@ -177,6 +234,18 @@ class DecodeServer:
             seq = self.running[b]
             seq[1] += 1
             seq[2] -= 1
+            seq[3] += 1
+            seq[4] = False
+            if seq[5]:                          # cut: the pages behind the kept tokens and the next one's go back
+                self.evicted += seq[1] - self.budget.keep
+                seq[1] = self.budget.keep
+                held = seq[1] // P + 1
+                if len(seq[0]) > held:
+                    self.pool.free_pages(seq[0][held:], done)
+                    if not self._held or self._held[-1] is not done:
+                        self._held.append(done)
+                    self.table[b, held: len(seq[0])] = -1
+                    del seq[0][held:]
             self.kv[b] = seq[1]
             if seq[2] == 0:
                 self._drop(b, done)
@@ -197,6 +266,27 @@ class DecodeServer:
                     continue
             b += 1
         return done, B, start
+
+    def _launch(self, B, max_kv):
+        """The step's calls, in order on the decode stream."""
+        step = dict(batch=B, kv_len=self.kv_dev, page_table=self.table_dev, max_pages=self.max_pages, max_kv_len=max_kv,
+                    token_ids=self.tok, x_out=self.x_out, logits=self.logits, next_token=None if self.sampling else self.nxt,
+                    stream=self.stream)
+        if self.budget is None:
+            self.ctx.decode_step(**step)
+        else:
+            position, arrived, after, keep, following = self.marks_dev
+            table = dict(batch=B, page_table=self.table_dev, max_pages=self.max_pages, track=self.track, stream=self.stream)
+            if any(seq[4] for seq in self.running):
+                self.ctx.kv_record_init(n_tokens=arrived, max_kv_len=max_kv, **table)
+            self.ctx.decode_step_tracked(track=self.track, position=position, decay=self.budget.decay, workspace=self.attend_ws, **step)
+        if self.sampling is not None:
+            with torch.cuda.stream(self.stream):
+                self.uniform.uniform_(generator=self.gen)
+            hb.sample(self.logits[:B], self.uniform, self.nxt, workspace=self.sample_ws, stream=self.stream, **self.settings)
+        if self.budget is not None and any(seq[5] for seq in self.running):
+            self.ctx.kv_evict(n_tokens=after, keep=keep, max_kv_len=max_kv, sink=self.budget.sink, recent=self.budget.recent,
+                              position=following, **table)
 
     def completed_steps(self):
         """[(tag, ms)] of the steps that have finished on the device since the last call, oldest first: `tag` is what
@@ -347,7 +437,7 @@ def replay(server: DecodeServer, arrivals, worker_factory=None, slo_ms=40.0, sam
            "tpot_ms_p99": float(np.percentile(tpot, 99)), "tpot_ms_max": float(tpot.max()), "within_slo": float(np.mean(tpot <= slo_ms)),
            "batch_mean": float(batches.mean()) if len(batches) else 0.0, "batch_max": int(batches.max()) if len(batches) else 0,
            "admitted": server.admitted, "finished": server.finished, "kv_admission_stalls": server.kv_stalls,
-           "preempted": server.preempted, "queued_at_end": len(server.queue), "snapshots": snaps,
+           "preempted": server.preempted, "queued_at_end": len(server.queue), "tokens_evicted": server.evicted, "snapshots": snaps,
            "plans": plans if plan is not None else [], "tpot_ms": tpot, "batches": batches, "step_ms": busy}
     if ft is not None:
         ft["tokens_per_s"] = ft["tokens"] / elapsed

@@ -1,0 +1,251 @@
+"""harli_kv_attend against the 64-bit oracle.
+
+Tolerances.  u = 2^-23 (one step of fp32, so that truncating adders count too).  A score is a sum of d products in some order, scaled
+before or after: off by at most delta = (d + 4) u sum_e |q_e k_e| / sqrt(d).  A probability then is off by a factor of at most
+exp(2 delta), times the roundings of two exponentials (2 u each), of sums of up to 256 terms in a chunk (lanes of at most 16 terms, then
+trees) and of up to `chunks` chunks, and of a division: (48 + chunks) u together.  Weights add at most n_q / n_kv probabilities to what was
+there (rounded twice).  Outputs add, for each value, as many roundings again."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import budget_oracle as O
+from paper_2511_11729_amd import binding as hb
+from tests.budget_util import DEV, P, CacheCase
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -23
+
+BF16_HEADS = [(4, 4, 64), (4, 2, 64), (8, 2, 64), (3, 3, 128), (4, 2, 128), (6, 2, 128), (8, 2, 128), (5, 1, 128), (12, 2, 128), (7, 1, 128), (8, 1, 128)]
+F32_HEADS = [(4, 4, 64), (6, 2, 48), (3, 1, 86), (2, 2, 300), (20, 2, 64), (4, 2, 130)]
+LENGTHS = [0, 1, 15, 16, 17, 127, 128, 129, 255, 256, 257, 700]
+
+
+def queries(case, seed=1, scale=2.0):
+    return np.random.default_rng(seed).normal(0, scale, (case.B, case.n_q, case.d)).astype(np.float32)
+
+
+def check(case, q, out, before, decay, layer=0, position=None):
+    rec, old = case.got_records(), before
+    touched = np.zeros(rec.shape, bool)
+    out = out.cpu().numpy().astype(np.float64)
+    for b in range(case.B):
+        n = int(case.n[b])
+        K, V = case.K[layer][b]
+        page, slot = case.slots(b, n)
+        ref, weight, prob = O.attend_weights(q[b], K, V, old["w"][layer, page, :, slot], decay, n - 1)
+        if n == 0:
+            assert np.all(out[b] == 0)
+            continue
+        group = case.n_q // case.n_kv
+        K_of, V_of = K.repeat(group, 1), V.repeat(group, 1)                      # [n, n_q, d]
+        delta = (case.d + 4) * U * (np.abs(q[b].astype(np.float64)) * np.abs(K_of)).sum(-1).max(0) / np.sqrt(case.d)
+        rel = np.expm1(2 * delta) + (48 + -(-n // 128)) * U                      # per query head
+        tiny = 2.0 ** -126                                                       # probabilities below the normal range may be zero
+        assert np.all(np.abs(out[b] - ref) <= 2 * rel[:, None] * (prob.T[..., None] * np.abs(V_of)).sum(0) + n * tiny), (b, n)
+        got = rec["w"][layer, page, :, slot].astype(np.float64)
+        bound = (rel[:, None] * prob).reshape(case.n_kv, group, n).sum(1).T + (group + 2) * U * np.abs(weight) + group * tiny
+        assert np.all(np.abs(got - weight) <= bound), (b, n)
+        pos = old["p"][layer, page, :, slot].copy()
+        pos[n - 1] = n - 1 if position is None else position[b]
+        assert np.array_equal(rec["p"][layer, page, :, slot], pos)
+        touched[layer, page, :, slot] = True
+    assert rec[~touched].tobytes() == old[~touched].tobytes()                    # every other record is as it was
+
+
+def run(case, decay=1.0, layer=0, position=None, **kw):
+    q = queries(case)
+    q_dev, out = torch.from_numpy(q).to(DEV), torch.full((case.B, case.n_q, case.d), float("nan"), device=DEV)
+    before = case.got_records()
+    pos = None if position is None else torch.from_numpy(np.asarray(position, np.int32)).to(DEV)
+    case.attend(q_dev, out, layer=layer, decay=decay, position=pos, **kw)
+    torch.cuda.synchronize()
+    case.ctx.check()
+    check(case, q, out, before, decay, layer, position)
+    return q_dev, out
+
+
+@pytest.mark.parametrize("heads", BF16_HEADS, ids=str)
+def test_bf16_head_layouts_at_the_edges_of_pages_and_chunks(heads):
+    run(CacheCase(LENGTHS, *heads))
+
+
+@pytest.mark.parametrize("heads", F32_HEADS, ids=str)
+def test_f32_head_layouts_at_the_edges_of_pages_and_chunks(heads):
+    run(CacheCase(LENGTHS, *heads, dtype="f32"))
+
+
+@pytest.mark.parametrize("dtype,heads", [("bf16", (8, 2, 128)), ("bf16", (7, 1, 128)), ("f32", (4, 2, 64))])
+@pytest.mark.parametrize("decay", [0.0, 0.75, 1.0])
+def test_decay_positions_and_layers(dtype, heads, decay):
+    case = CacheCase([40, 1, 300], *heads, dtype=dtype, layers=3)
+    if decay == 0.0:                       # what was there is not looked at
+        case.records["w"][...] = np.nan
+        case.reset()
+    run(case, decay=decay, layer=1, position=[1000, 5, 70000])
+    run(case, decay=decay, layer=2)
+
+
+@pytest.mark.parametrize("lengths", [[5000], [1] * 70, [3000, 2] * 8, [0, 0, 0]])
+def test_long_short_and_empty_sequences(lengths):
+    run(CacheCase(lengths, 8, 2, 128))
+    run(CacheCase(lengths, 3, 1, 86, dtype="f32"))
+
+
+def test_large_and_small_scores_stay_finite():
+    """Scores of +-1000: all weight on one token, every other probability underflows."""
+    case = CacheCase([33, 400], 4, 4, 64, poison=False)
+    q = queries(case, scale=1000.0)
+    out = torch.empty(case.B, case.n_q, case.d, device=DEV)
+    before = case.got_records()
+    case.attend(torch.from_numpy(q).to(DEV), out, decay=0.0)
+    torch.cuda.synchronize()
+    for b in range(case.B):
+        n = int(case.n[b])
+        ref, weight, prob = O.attend_weights(q[b], *case.K[0][b], before["w"][0, case.slots(b, n)[0], :, case.slots(b, n)[1]], 0.0, n)
+        clear = np.sort(prob, 1)[:, -1] > 1 - 1e-12                              # heads whose score differences dwarf their error
+        assert np.all(np.isfinite(out[b].cpu().numpy()))
+        assert clear.any() and np.allclose(out[b].cpu().numpy()[clear], ref[clear], rtol=1e-6, atol=1e-6)
+
+
+def test_without_records_the_output_has_the_same_bits():
+    case = CacheCase(LENGTHS, 8, 2, 128)
+    q, out = run(case)
+    again = torch.empty_like(out)
+    before = case.track.clone()
+    case.attend(q, again, track=False)
+    torch.cuda.synchronize()
+    assert torch.equal(out, again) and torch.equal(before, case.track)
+
+
+@pytest.mark.parametrize("dtype,heads", [("bf16", (8, 2, 128)), ("bf16", (7, 1, 128)), ("bf16", (4, 4, 64)), ("f32", (4, 2, 64))])
+def test_the_same_call_gives_the_same_bits_captured_and_replayed(dtype, heads):
+    case = CacheCase([300, 17, 0, 1000], *heads, dtype=dtype)
+    q = torch.from_numpy(queries(case)).to(DEV)
+    out, eager = torch.empty_like(q), torch.empty_like(q)
+    case.attend(q, eager)
+    torch.cuda.synchronize()
+    want = case.track.clone()
+    case.reset()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        case.attend(q, out, stream=torch.cuda.current_stream())
+    start = case.track.clone()
+    for _ in range(3):
+        case.track.copy_(start)
+        out.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager) and torch.equal(case.track, want)
+
+
+def test_calls_on_two_streams_with_workspaces_apart():
+    a, b = CacheCase([700, 30], 8, 2, 128, seed=1), CacheCase([650, 90], 8, 2, 128, seed=2)
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    outs = []
+    for case, st in zip((a, b), streams):
+        q = torch.from_numpy(queries(case)).to(DEV)
+        outs.append((q, torch.empty_like(q), case.got_records()))
+    torch.cuda.synchronize()
+    for case, st, (q, out, _) in zip((a, b), streams, outs):
+        case.attend(q, out, stream=st)
+    torch.cuda.synchronize()
+    for case, (q, out, before) in zip((a, b), outs):
+        check(case, q.cpu().numpy(), out, before, 1.0)
+
+
+def test_far_pages_of_a_cache_beyond_four_gigabytes():
+    """Page offsets and record offsets past 32 bits: the sequence lies in the last chunks of a 9 GB slab."""
+    n_kv, d, block = 2, 128, 2 << 20
+    ppb, chunks = block // (P * n_kv * d * 2), 2200
+    slab = torch.zeros(chunks * 2 * block, dtype=torch.uint8, device=DEV)
+    pool = hb.Pool(slab, slab.numel(), block_bytes=block, n_layers=1, kv_row_bytes=n_kv * d * 2)
+    near = CacheCase([90], 4, n_kv, d)
+    ctx = hb.Context(pool, n_layers=1, hidden=16, n_q_heads=4, n_kv_heads=n_kv, head_dim=d, ffn=16, max_batch=1, max_seq_len=90, layers=[near.layer])
+    shift = chunks * ppb - near.n_pages
+    far = torch.as_strided(slab.view(torch.bfloat16), (chunks, 1, 2, ppb, n_kv, P, d), (block, block, block // 2, P * n_kv * d, P * d, d, 1))
+    table = torch.from_numpy(np.where(near.table >= 0, near.table + shift, -1).astype(np.int32)).to(DEV)
+    for page in near.table[near.table >= 0].tolist():
+        far[(page + shift) // ppb, 0, :, (page + shift) % ppb] = near.view[page // near.ppb, 0, :, page % near.ppb]
+    records = torch.zeros(1, chunks * ppb, n_kv, P, 2, dtype=torch.int32, device=DEV)
+    records[:, shift:] = near.track
+    q = torch.from_numpy(queries(near)).to(DEV)
+    out, out_near = torch.empty_like(q), torch.empty_like(q)
+    near.attend(q, out_near)
+    ctx.kv_attend(layer=0, batch=1, q=q, out=out, n_tokens=near.n_dev, page_table=table, max_pages=near.max_pages, max_kv_len=90, track=records,
+                  workspace=near.workspace)
+    torch.cuda.synchronize()
+    ctx.check()
+    assert torch.equal(out, out_near) and torch.equal(records[:, shift:], near.track)
+    assert int(records[:, :shift].count_nonzero()) == 0
+
+
+def test_records_of_a_prompt():
+    case = CacheCase([0, 5, 16, 100], 8, 2, 128, layers=2)
+    before = case.got_records()
+    case.ctx.kv_record_init(batch=case.B, n_tokens=case.n_dev, page_table=case.table_dev, max_pages=case.max_pages, max_kv_len=case.longest, track=case.track)
+    torch.cuda.synchronize()
+    case.ctx.check()
+    want = before.copy()
+    for b in range(case.B):
+        page, slot = case.slots(b, int(case.n[b]))
+        want["w"][:, page, :, slot] = 0
+        want["p"][:, page, :, slot] = np.arange(int(case.n[b]))[:, None, None]
+    assert case.got_records().tobytes() == want.tobytes()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_bad_pages_and_too_long_sequences_are_reported_and_do_no_harm(dtype):
+    case = CacheCase([100, 40, 70], 8, 2, 128 if dtype == "bf16" else 64, dtype=dtype)
+    q = torch.from_numpy(queries(case)).to(DEV)
+    out, good = torch.empty_like(q), torch.empty_like(q)
+    case.attend(q, good)
+    torch.cuda.synchronize()
+    want = case.got_records()
+    for page in (10_000_000, -5):
+        case.reset()
+        case.table_dev[0, 2] = page
+        case.attend(q, out)
+        torch.cuda.synchronize()
+        with pytest.raises(hb.HarliError, match="page id"):
+            case.ctx.check()
+        assert torch.equal(out[1:], good[1:]) and torch.isfinite(out[0]).all()
+        rec = case.got_records()
+        for b in (1, 2):
+            page_, slot = case.slots(b, int(case.n[b]))
+            assert rec[0, page_, :, slot].tobytes() == want[0, page_, :, slot].tobytes()
+    case.reset()
+    case.n_dev[1] = case.max_pages * P + 1
+    case.attend(q, out)
+    torch.cuda.synchronize()
+    with pytest.raises(hb.HarliError, match="longer"):
+        case.ctx.check()
+    assert torch.equal(out[0], good[0]) and torch.equal(out[2], good[2])
+    case.ctx.check()
+
+
+def test_refusals():
+    case = CacheCase([20, 30], 8, 2, 128)
+    q = torch.zeros(2, 8, 128, device=DEV)
+    out = torch.full_like(q, 7.0)
+    before = case.track.clone()
+    bad = [dict(batch=0), dict(batch=3), dict(layer=-1), dict(layer=1), dict(q=None), dict(out=None), dict(n_tokens=None), dict(page_table=None),
+           dict(max_kv_len=0), dict(max_kv_len=31), dict(max_pages=1), dict(decay=-0.1), dict(decay=1.5), dict(decay=float("nan")),
+           dict(workspace=None), dict(workspace=case.workspace[:-1]), dict(workspace=case.workspace[64:]), dict(q=q.data_ptr() + 4),
+           dict(out=out.data_ptr() + 8), dict(track=case.track.data_ptr() + 8), dict(max_pages=(1 << 26) + 1)]
+    for kw in bad:
+        args = dict(layer=0, batch=2, q=q, out=out, n_tokens=case.n_dev, page_table=case.table_dev, max_pages=case.max_pages, max_kv_len=30,
+                    track=case.track, workspace=case.workspace)
+        with pytest.raises(hb.HarliError) as e:
+            case.ctx.kv_attend(**dict(args, **kw))
+        assert e.value.status == hb.HARLI_ERR_INVALID, kw
+    for kw in (dict(batch=0), dict(batch=3), dict(n_tokens=None), dict(page_table=None), dict(track=None), dict(track=case.track.data_ptr() + 8),
+               dict(max_kv_len=0), dict(max_kv_len=31), dict(max_pages=1), dict(max_pages=(1 << 26) + 1)):
+        args = dict(batch=2, n_tokens=case.n_dev, page_table=case.table_dev, max_pages=case.max_pages, max_kv_len=30, track=case.track)
+        with pytest.raises(hb.HarliError) as e:
+            case.ctx.kv_record_init(**dict(args, **kw))
+        assert e.value.status == hb.HARLI_ERR_INVALID, kw
+    assert case.ctx.kv_attend_workspace_bytes(3, 10) == 0 and case.ctx.kv_attend_workspace_bytes(1, 31) == 0
+    torch.cuda.synchronize()
+    case.ctx.check()
+    assert bool((out == 7).all()) and torch.equal(before, case.track)

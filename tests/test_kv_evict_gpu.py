@@ -1,0 +1,166 @@
+"""harli_kv_evict against the oracle: which rows move is a matter of order alone, so every byte of the cache and of the records has to be
+the oracle's."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import budget_oracle as O
+from paper_2511_11729_amd import binding as hb
+from tests.budget_util import DEV, CacheCase
+
+pytestmark = pytest.mark.gpu
+
+
+def expected(case, keep, sink=0, recent=0, position=None):
+    """(cache, records) after the eviction, in bits."""
+    cache = case.cache.view(torch.int32 if case.dtype == "f32" else torch.int16).clone()
+    old, rec = cache.clone(), case.records.copy()
+    moved = 0
+    for b in range(case.B):
+        n = int(case.n[b])
+        page, slot = case.slots(b, n)
+        for l in range(case.L):
+            for c in range(case.n_kv):
+                r = case.records[l, page, c, slot]
+                moves = O.evict_moves(r["w"], r["p"], keep[b], n if position is None else position[b], sink, recent)
+                for a, t in moves:
+                    cache[page[t] // case.ppb, l, :, page[t] % case.ppb, c, slot[t]] = old[page[a] // case.ppb, l, :, page[a] % case.ppb, c, slot[a]]
+                    rec[l, page[t], c, slot[t]] = case.records[l, page[a], c, slot[a]]
+                moved += len(moves)
+    return cache, rec, moved
+
+
+def run(case, keep, position=None, **kw):
+    want, rec, moved = expected(case, keep, position=position, **kw)
+    left = torch.full((case.B,), -9, dtype=torch.int32, device=DEV)
+    pos = None if position is None else torch.from_numpy(np.asarray(position, np.int32)).to(DEV)
+    case.evict(keep, position=pos, n_left=left, **kw)
+    torch.cuda.synchronize()
+    case.ctx.check()
+    assert torch.equal(case.view.cpu().view(want.dtype), want)
+    assert case.got_records().tobytes() == rec.tobytes()
+    assert left.tolist() == [min(int(n), max(int(k), 0)) for n, k in zip(case.n, keep)]
+    return moved
+
+
+@pytest.mark.parametrize("dtype,heads", [("bf16", (4, 4, 64)), ("bf16", (2, 2, 128)), ("f32", (2, 2, 64)), ("f32", (3, 1, 86)), ("f32", (2, 2, 6))])
+@pytest.mark.parametrize("sink,recent", [(0, 0), (4, 16)])
+def test_ragged_batch(dtype, heads, sink, recent):
+    case = CacheCase([0, 1, 15, 16, 17, 64, 65, 200, 300, 1040], *heads, dtype=dtype, layers=2)
+    assert run(case, [5, 0, 15, 3, 16, 63, 1, 100, 299, 1024], sink=sink, recent=recent) > 100
+
+
+@pytest.mark.parametrize("n,keep", [(255, 1), (256, 255), (257, 128), (1000, 0), (1000, 999), (1000, 1000), (1000, 5000), (1000, -3), (2049, 1025), (7000, 3500), (20001, 10000), (40007, 25000)])
+def test_lengths_across_the_sizes_of_the_search(n, keep):
+    run(CacheCase([n, max(1, n // 3)], 1, 1, 64), [keep, keep // 3], sink=2, recent=min(20, n))
+
+
+def test_more_moves_than_one_list_holds():
+    """The heavy tokens all lie behind the kept length: every slot is refilled."""
+    case = CacheCase([9000], 1, 1, 64)
+    page, slot = case.slots(0, 9000)
+    case.records["w"][0, page, 0, slot] = np.arange(9000)
+    case.reset()
+    assert run(case, [4500]) == 4500
+
+
+@pytest.mark.parametrize("weights", ["equal", "zeros", "few", "signed", "nan", "inf"])
+def test_ties_and_strange_weights(weights):
+    case = CacheCase([300, 77], 2, 2, 64)
+    r = np.random.default_rng(3)
+    shape = case.records.shape
+    w = {"equal": np.full(shape, 0.25), "zeros": np.where(r.random(shape) < 0.5, 0.0, -0.0), "few": r.integers(0, 3, shape) / 4,
+         "signed": r.normal(size=shape), "nan": np.where(r.random(shape) < 0.4, np.nan, r.random(shape)),
+         "inf": np.where(r.random(shape) < 0.3, np.inf, np.where(r.random(shape) < 0.3, -np.inf, 1.0))}[weights]
+    case.records["w"] = w
+    if weights == "nan":
+        case.records["w"].view(np.int32)[r.random(shape) < 0.1] = -1            # a NaN with every bit set
+    case.reset()
+    run(case, [150, 60], sink=1, recent=7)
+
+
+def test_protected_tokens_beyond_what_is_kept_and_positions_in_any_order():
+    case = CacheCase([200, 120], 2, 2, 128)
+    r = np.random.default_rng(5)
+    case.records["p"] = r.integers(0, 5000, case.records.shape)
+    case.reset()
+    run(case, [40, 80], sink=100, recent=4500, position=[5000, 5000])
+    case.reset()
+    run(case, [40, 80], sink=0, recent=2500, position=[5000, 2 ** 31 - 1])
+    case.reset()
+    run(case, [100, 80], sink=0, recent=2 ** 31 - 1, position=[0, -5])
+
+
+def test_steps_of_one_page_after_another():
+    """Evicted again and again, as a service does; each time the oracle starts from what is there."""
+    case = CacheCase([200, 150], 4, 2, 128, layers=2)
+    keep = [184, 140]
+    for _ in range(4):
+        run(case, keep, sink=2, recent=8)
+        case.cache = case.view.cpu().clone()
+        case.records = case.got_records().copy()
+        case.n = np.minimum(case.n, keep).astype(np.int32)
+        case.reset()
+        keep = [k - 16 for k in keep]
+
+
+def test_captured_and_replayed():
+    case = CacheCase([300, 64, 1000], 2, 2, 128)
+    keep = [100, 60, 1000]
+    want, rec, _ = expected(case, keep, sink=1, recent=3)
+    case.evict(keep, sink=1, recent=3)                       # the arguments' tensors live on in the case
+    case.reset()
+    g = torch.cuda.CUDAGraph()
+    track, cache = case.track.clone(), case.view.clone()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        case.ctx.kv_evict(batch=case.B, n_tokens=case.n_dev, keep=case.keep_dev, page_table=case.table_dev, max_pages=case.max_pages,
+                          max_kv_len=case.longest, track=case.track, sink=1, recent=3, stream=torch.cuda.current_stream())
+    for _ in range(3):
+        case.track.copy_(track)
+        case.view.copy_(cache)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(case.view.cpu().view(want.dtype), want) and case.got_records().tobytes() == rec.tobytes()
+
+
+def test_bad_pages_and_too_long_sequences_are_reported_and_other_sequences_are_right():
+    case = CacheCase([100, 64, 90], 2, 2, 64)
+    keep = [50, 30, 45]
+    want, rec, _ = expected(case, keep)
+    pages = {b: case.slots(b, int(case.n[b])) for b in range(3)}
+    case.table_dev[1, 2] = 1 << 30
+    case.evict(keep)
+    torch.cuda.synchronize()
+    with pytest.raises(hb.HarliError, match="page id"):
+        case.ctx.check()
+    got = case.got_records()
+    for b in (0, 2):
+        page, slot = pages[b]
+        assert got[0, page, :, slot].tobytes() == rec[0, page, :, slot].tobytes()
+        assert torch.equal(case.view.cpu().view(want.dtype)[page // case.ppb, 0, :, page % case.ppb, :, slot], want[page // case.ppb, 0, :, page % case.ppb, :, slot])
+    case.reset()
+    case.n_dev[0] = case.longest + 1
+    left = torch.zeros(3, dtype=torch.int32, device=DEV)
+    case.evict(keep, n_left=left)
+    torch.cuda.synchronize()
+    with pytest.raises(hb.HarliError, match="longer"):
+        case.ctx.check()
+    page, slot = pages[0]
+    assert case.got_records()[0, page, :, slot].tobytes() == case.records[0, page, :, slot].tobytes()
+    assert left.tolist() == [case.longest + 1, 30, 45]
+
+
+def test_refusals():
+    case = CacheCase([20, 30], 2, 2, 64)
+    keep = torch.tensor([5, 5], dtype=torch.int32, device=DEV)
+    good = dict(batch=2, n_tokens=case.n_dev, keep=keep, page_table=case.table_dev, max_pages=case.max_pages, max_kv_len=30, track=case.track)
+    for kw in (dict(batch=0), dict(batch=3), dict(n_tokens=None), dict(keep=None), dict(page_table=None), dict(track=None), dict(max_kv_len=0),
+               dict(max_kv_len=31), dict(max_pages=1), dict(sink=-1), dict(recent=-1), dict(n_left=keep), dict(n_left=case.n_dev),
+               dict(track=case.track.data_ptr() + 8), dict(max_pages=(1 << 26) + 1)):
+        with pytest.raises(hb.HarliError) as e:
+            case.ctx.kv_evict(**dict(good, **kw))
+        assert e.value.status == hb.HARLI_ERR_INVALID, kw
+    torch.cuda.synchronize()
+    case.ctx.check()
+    assert case.got_records().tobytes() == case.records.tobytes()

@@ -1,0 +1,192 @@
+"""harli_sample against the 64-bit oracle.
+
+A token is a whole number and has to be the oracle's, unless the random number lies on a border of the distribution: within 1e-9 of a
+border between two tokens, where rounding of either side decides (weights are fixed point with at least 38 bits below the largest, their
+sums exact), the neighbour is right too.  The log probability is off by at most half a step of fp32, plus 1e-9 for the weights."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import budget_oracle as O
+from paper_2511_11729_amd import binding as hb
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def sample(logits, uniform, ld=None, stream=None, **settings):
+    B, V = logits.shape
+    ld = ld or V
+    rows = torch.full((B, ld), 1e30, device=DEV)             # what lies between the rows is larger than every logit
+    rows[:, :V] = torch.from_numpy(logits).to(DEV)
+    dev = {k: torch.from_numpy(np.asarray(v, np.int32 if k == "top_k" else np.float32)).to(DEV) for k, v in settings.items()}
+    token = torch.full((B,), -99, dtype=torch.int32, device=DEV)
+    logprob = torch.full((B,), 99.0, device=DEV)
+    ws = torch.empty(hb.sample_workspace_bytes(B, V), dtype=torch.uint8, device=DEV)
+    hb.sample(rows[:, :V], torch.from_numpy(np.asarray(uniform, np.float32)).to(DEV), token, logprob=logprob, workspace=ws, stream=stream, **dev)
+    torch.cuda.synchronize()
+    return token.cpu().numpy(), logprob.cpu().numpy()
+
+
+def check(logits, uniform, ld=None, **settings):
+    token, logprob = sample(logits, uniform, ld, **settings)
+    uniform = np.asarray(uniform, np.float32).astype(np.float64)
+    for b, row in enumerate(logits):
+        kw = {k: (int(v[b]) if k == "top_k" else float(np.float32(v[b]))) for k, v in settings.items()}
+        want, lp = O.sample_token(row, uniform[b], **kw)
+        if token[b] != want:
+            kept, weight = O.sample_kept(row, **kw)
+            by = sorted(zip(kept, weight))
+            total = math.fsum(w for _, w in by)
+            near = {O.sample_token(row, min(max(uniform[b] + e, 0.0), 1 - 1e-16), **kw)[0] for e in (-1e-9, 1e-9)}
+            assert int(token[b]) in near, (b, int(token[b]), want, kw)
+            lp = math.log(dict(by)[int(token[b])] / total)
+        if math.isinf(lp):
+            assert logprob[b] == lp
+        else:
+            assert abs(logprob[b] - lp) <= 2.0 ** -24 * abs(lp) + 2e-9, (b, logprob[b], lp)
+    return token
+
+
+def rows(B, V, seed=0, spread=2.5):
+    r = np.random.default_rng(seed)
+    z = r.normal(0, spread, (B, V)).astype(np.float32)
+    for b in range(B):
+        z[b, r.integers(0, V, max(1, V // 50))] += np.float32(r.uniform(2, 9))
+    return z, r
+
+
+def mixed(B, V, r):
+    return dict(temperature=r.uniform(0.3, 2.0, B), top_k=r.choice([0, 1, 2, 5, 50, V - 1, V, V + 7, -3], B),
+                top_p=r.choice([1.0, 0.0, -1.0, 0.1, 0.5, 0.9, 0.999, 2.0], B), min_p=r.choice([0.0, -1.0, 0.01, 0.2, 1.0], B))
+
+
+@pytest.mark.parametrize("V", [1, 2, 3, 63, 64, 65, 255, 1000, 1023, 1025, 4097])
+def test_every_filter_at_small_vocabularies(V):
+    z, r = rows(24, V, V)
+    check(z, r.random(24))
+    for name, v in mixed(24, V, r).items():
+        check(z, r.random(24), **{name: v})
+    check(z, r.random(24), ld=V + 5, **mixed(24, V, r))
+
+
+@pytest.mark.parametrize("V,B", [(8000, 6), (32000, 5), (50257, 3), (128256, 3), (152064, 2)])
+def test_vocabularies_of_models(V, B):
+    z, r = rows(B, V, V)
+    check(z, r.random(B))
+    check(z, r.random(B), temperature=np.full(B, 0.7), top_k=np.full(B, 40))
+    check(z, r.random(B), temperature=np.full(B, 1.3), top_p=np.full(B, 0.9))
+    check(z, r.random(B), min_p=np.full(B, 0.05))
+    check(z, r.random(B), ld=V + 3, temperature=np.full(B, 1.0), top_k=np.full(B, 500), top_p=np.full(B, 0.95), min_p=np.full(B, 0.001))
+
+
+@pytest.mark.parametrize("levels", [1, 2, 7, 40])
+def test_equal_logits_go_by_index(levels):
+    """Logits on a few levels: every cut falls inside a run of equal ones."""
+    r = np.random.default_rng(levels)
+    z = (r.integers(0, levels, (20, 3000)) / 4.0).astype(np.float32)
+    z[::2] = np.where(z[::2] == 0, np.where(r.random(z[::2].shape) < 0.5, 0.0, -0.0), z[::2])
+    check(z, r.random(20), top_k=r.integers(1, 3000, 20))
+    check(z, r.random(20), top_p=r.random(20))
+    check(z, r.random(20), top_k=r.integers(1, 3000, 20), top_p=r.random(20), temperature=r.uniform(0.1, 3, 20))
+    assert np.array_equal(check(z, r.random(20), temperature=np.zeros(20)), z.argmax(1))
+
+
+def test_masks_infinities_and_nan():
+    z, r = rows(12, 500, 4)
+    z[0] = -np.inf
+    z[1, 1:] = -np.inf
+    z[2, ::2] = -np.inf
+    z[3] = np.finfo(np.float32).min
+    z[4, 100:] = np.finfo(np.float32).min
+    z[5, 7], z[5, 9] = np.inf, np.inf
+    z[6, ::3] = np.nan
+    z[7] = np.nan
+    z[8, 3] = np.finfo(np.float32).max
+    z[9, :499] = -np.inf
+    z[10, 10:] = np.nan
+    for seed in range(3):
+        u = np.random.default_rng(seed).random(12)
+        check(z, u)
+        check(z, u, **mixed(12, 500, np.random.default_rng(seed + 9)))
+        check(z, u, temperature=np.full(12, np.inf))
+        check(z, u, temperature=np.full(12, 1e-30))
+        check(z, u, temperature=np.full(12, 1e-45))
+        check(z, u, top_k=np.full(12, 300), top_p=np.full(12, 0.7))
+    assert check(z, r.random(12), temperature=np.full(12, np.nan))[0] == -1
+
+
+@pytest.mark.parametrize("u", [0.0, -0.0, -1.0, float("nan"), 1.0, 2.0, float("inf"), np.nextafter(np.float32(1), np.float32(0)), 1e-30, 1e-45])
+def test_random_numbers_at_and_past_the_ends(u):
+    z, r = rows(6, 900, 2)
+    settings = mixed(6, 900, r)
+    token, _ = sample(z, np.full(6, u, np.float32), **settings)
+    for b in range(6):
+        kept, w = O.sample_kept(z[b], **{k: (int(v[b]) if k == "top_k" else float(np.float32(v[b]))) for k, v in settings.items()})
+        assert token[b] == (max(i for i, x in zip(kept, w) if x > 2.0 ** -50) if u >= 1 else O.sample_token(z[b], u, **{
+            k: (int(v[b]) if k == "top_k" else float(np.float32(v[b]))) for k, v in settings.items()})[0])
+
+
+def test_settings_that_are_not_a_number_are_off():
+    z, r = rows(4, 700, 6)
+    u = r.random(4)
+    nan = np.full(4, np.nan)
+    a, b = sample(z, u), sample(z, u, top_p=nan, min_p=nan)
+    assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+
+
+def test_the_draws_follow_the_distribution():
+    """4096 rows of the same logits and evenly spaced random numbers: each token is drawn as often as its share says, to one row."""
+    r = np.random.default_rng(0)
+    z = r.normal(0, 1.5, 37).astype(np.float32)
+    n = 4096
+    token, _ = sample(np.tile(z, (n, 1)), (np.arange(n) + 0.5) / n, temperature=np.full(n, 0.8), top_k=np.full(n, 20))
+    kept, w = O.sample_kept(z, temperature=float(np.float32(0.8)), top_k=20)
+    share = np.zeros(37)
+    share[kept] = np.asarray(w) / math.fsum(w)
+    assert np.all(np.abs(np.bincount(token, minlength=37) - share * n) <= 1.0 + 1e-6)
+
+
+def test_the_same_row_gives_the_same_token_in_any_batch_and_captured():
+    z, r = rows(40, 32000, 8)
+    settings = mixed(40, 32000, r)
+    u = r.random(40)
+    token, logprob = sample(z, u, **settings)
+    for b in range(0, 40, 7):
+        t, lp = sample(z[b: b + 1], u[b: b + 1], **{k: v[b: b + 1] for k, v in settings.items()})
+        assert t[0] == token[b] and lp[0] == logprob[b]
+    zd, ud = torch.from_numpy(z).to(DEV), torch.from_numpy(u.astype(np.float32)).to(DEV)
+    dev = {k: torch.from_numpy(np.asarray(v, np.int32 if k == "top_k" else np.float32)).to(DEV) for k, v in settings.items()}
+    out, lp = torch.empty(40, dtype=torch.int32, device=DEV), torch.empty(40, device=DEV)
+    ws = torch.empty(hb.sample_workspace_bytes(40, 32000), dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        hb.sample(zd, ud, out, logprob=lp, workspace=ws, stream=torch.cuda.current_stream(), **dev)
+    for _ in range(3):
+        out.fill_(-5)
+        ws.fill_(0x5a)                                       # whatever is in the workspace
+        g.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(out.cpu().numpy(), token) and np.array_equal(lp.cpu().numpy(), logprob)
+
+
+def test_two_streams_with_workspaces_apart():
+    z, r = rows(8, 32000, 9)
+    u = r.random(8)
+    want = sample(z, u, top_p=np.full(8, 0.9))
+    outs = []
+    zd, ud, p = torch.from_numpy(z).to(DEV), torch.from_numpy(u.astype(np.float32)).to(DEV), torch.full((8,), 0.9, device=DEV)
+    torch.cuda.synchronize()
+    for _ in range(2):
+        st = torch.cuda.Stream()
+        token, ws = torch.empty(8, dtype=torch.int32, device=DEV), torch.empty(hb.sample_workspace_bytes(8, 32000), dtype=torch.uint8, device=DEV)
+        outs.append((token, ws, st))
+    torch.cuda.synchronize()
+    for token, ws, st in outs:
+        hb.sample(zd, ud, token, top_p=p, workspace=ws, stream=st)
+    torch.cuda.synchronize()
+    for token, _, _ in outs:
+        assert np.array_equal(token.cpu().numpy(), want[0])
