@@ -383,14 +383,14 @@ harli_status harli_kv_evict(harli_ctx* c, const harli_evict_batch* b, void* hip_
  *   top-p   keeps, of those, each one for which the weights before it add up to less than p times the weight of the k;
  *   min-p   keeps w_i >= min_p (times the largest weight, which is 1);
  *   token   = the first index i, by index, at which the kept weights up to i add up to more than uniform times their sum.
- * The first token in order always stays.  Weights are held in fixed point with 62 bits for a row's sum: a weight below 2^-38 or less
- * (2^-44 at 152064 tokens) of the largest may be never drawn, and the result does not depend on how the work was split.
+ * The first token in order always stays.  Weights are rounded to fixed point: one below 2^-51 of the largest among its 4096 neighbours
+ * (indexes 4096 k to 4096 k + 4095) is never drawn.  A row's result depends neither on the batch nor on the run.
  * temperature <= 0 or NaN: the first token in order.  A logit of -inf or NaN is never drawn; several of +inf share the row.
  * A row without a token that can be drawn gets token -1, logprob -inf.
  * ======================================================================== */
 typedef struct {
-  int32_t batch;             /* >= 1 */
-  int32_t vocab;             /* 1..2^24 */
+  int32_t batch;             /* 1..65535 */
+  int32_t vocab;             /* 1..2^20 */
   const float* logits;       /* device, row b at logits + b * ld */
   int64_t ld;                /* >= vocab */
   const float* uniform;      /* device [batch], [0, 1): below 0 or NaN counts as 0, from 1 on draws the last */

@@ -1,211 +1,643 @@
 // A token per row of logits by temperature, top-k, top-p and min-p (harli_sample).
-// All three filters keep the first tokens in the order of (logit, then lower index), so what stays is a cut: a logit and how many of
-// the tokens that have just this logit.  The cut is found digit by digit on the logits' order-preserving integers, counting tokens
-// for top-k and adding weights for top-p.  Weights are exp in 64 bits, rounded to fixed point: their sums are the same in any order.
+//
+// All three filters keep the first tokens in the order of (logit, then lower index), so what stays is a cut: a logit, and the last index
+// among the tokens that have just this logit.  Two launches:
+//   k_sample_stretch  reads the logits once, kStretch of a row per workgroup, all in registers: their maximum, the sum of their weights
+//                     (relative to that maximum) and, where a filter asks for it, tokens and weights by bins of the logit;
+//   k_sample_row      one workgroup per row: puts the stretches together, finds the bin that a cut falls into, fetches the tokens of that
+//                     bin (only from stretches that have some) and settles the cut among them in LDS; then the stretch that the random
+//                     number points at, and the token in it.
+// Weights are exp in 64 bits rounded to fixed point, so sums by atomics are the same in any order; stretches are joined in 64-bit floating
+// point in a fixed order.  A row's result depends neither on the batch nor on scheduling.
+// What bounds it: HBM for the logits in the first launch, with the exponential in 64 bits close behind it (20 instructions per token: 20 us for
+// 256 rows of 152064 against 26 us of reading); in the second the latency of its steps.
+#include <mutex>
+
 #include "ctx.h"
 #include "device_utils.h"
 
 namespace harli {
 namespace {
 
-constexpr int kSampleThreads = 1024;
 typedef unsigned long long u64;
+constexpr int kStretch = 4096;      // tokens per workgroup of the first launch: sixteen per thread
+constexpr int kMostVocab = 1 << 20;  // 256 stretches
+constexpr int kMostStretches = kMostVocab / kStretch;
+constexpr int kLogitBins = 256;     // of a stretch, downwards from its maximum
+constexpr int kCandidates = 8192;   // tokens of one bin that the second launch holds in LDS
+constexpr int kDigits = 2048;       // bins of a search: 11 bits
+constexpr int kRowThreads = 1024, kRowWaves = kRowThreads / 64;
+constexpr double kOne = (double)(1ull << 50);  // weight 1 in fixed point: 2^12 of them and more fit 64 bits
 
-__device__ __forceinline__ unsigned order_key(float v) {  // of a logit that is not NaN; both zeros alike
+// Order of the logits as unsigned integers; both zeros alike.
+__device__ __forceinline__ unsigned order_key(float v) {
   const unsigned u = __float_as_uint(v + 0.f);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float order_value(unsigned k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+__device__ __forceinline__ bool usable(float v) { return v > -INFINITY; }  // (not NaN either)
 
-// exp((v - max) / t) in fixed point (`one` stands for 1)
-__device__ __forceinline__ double weight_of(float v, float max, double inv_t) {
-  return v == max ? 1.0 : v == -INFINITY || max == INFINITY ? 0.0 : exp(((double)v - (double)max) * inv_t);
+// 2^t for t <= 0: t = n + f, the series of 2^f = exp(f ln 2) over |f| <= 1/2 to the eleventh power (what follows is below 7e-15)
+__device__ __forceinline__ double exp2_series(double t) {
+  constexpr double l = 0.693147180559945309417;
+  constexpr double c1 = l, c2 = c1 * l / 2, c3 = c2 * l / 3, c4 = c3 * l / 4, c5 = c4 * l / 5, c6 = c5 * l / 6, c7 = c6 * l / 7, c8 = c7 * l / 8,
+                   c9 = c8 * l / 9, c10 = c9 * l / 10, c11 = c10 * l / 11;
+  t = fmax(t, -1080.0);  // zero in any case
+  const double n = rint(t), f = t - n;
+  double p = c11;
+  p = fma(p, f, c10), p = fma(p, f, c9), p = fma(p, f, c8), p = fma(p, f, c7), p = fma(p, f, c6), p = fma(p, f, c5), p = fma(p, f, c4);
+  p = fma(p, f, c3), p = fma(p, f, c2), p = fma(p, f, c1), p = fma(p, f, 1.0);
+  return __builtin_amdgcn_ldexp(p, (int)n);
 }
-__device__ __forceinline__ u64 fixed_of(double w, double one) { return (u64)(w * one + 0.5); }
+// weight of a usable logit, relative to `top`; per_t = log2(e) / temperature
+__device__ __forceinline__ double weight_of(float v, float top, double per_t) {
+  return v == top ? 1.0 : top == INFINITY || v == -INFINITY ? 0.0 : exp2_series(((double)v - (double)top) * per_t);
+}
+__device__ __forceinline__ u64 fixed_of(double w) {  // w <= 1: added to 2^52, its integer part stands in the low bits, rounded
+  return (u64)__double_as_longlong(fma(w, kOne, (double)(1ull << 52))) & ((1ull << 52) - 1);
+}
+
+// Bins of the logit for a row: their width is an eighth of the temperature, within 1/16 and 1/8 of the logit's unit, so that 256 of them span 16
+// units at least and one holds a few per cent of a vocabulary at most.  They lie on a grid common to all stretches.
+__device__ __forceinline__ float bins_per_unit(float t) { return fminf(fmaxf(8.f / t, 8.f), 16.f); }
+__device__ __forceinline__ int bin_of(float v, float per_unit) {  // monotone; kept inside the integers
+  return (int)floorf(fminf(fmaxf(v * per_unit, -5e8f), 5e8f));
+}
+
+struct RowSettings {
+  float t, p;
+  double min_p;
+  int k;  // 0: off
+  bool greedy, cut;
+};
+__device__ __forceinline__ RowSettings settings_of(const harli_sample_batch& a, int b) {
+  RowSettings s;
+  s.t = a.temperature ? a.temperature[b] : 1.f;
+  s.greedy = !(s.t > 0.f);
+  s.k = a.top_k ? a.top_k[b] : 0;
+  if (s.k < 0 || s.k >= a.vocab) s.k = 0;
+  s.p = a.top_p ? a.top_p[b] : 1.f;
+  if (!(s.p < 1.f)) s.p = 1.f;
+  const float m = a.min_p ? a.min_p[b] : 0.f;
+  s.min_p = m > 1.f ? 1.0 : m > 0.f ? (double)m : 0.0;
+  s.cut = !s.greedy && (s.k > 0 || s.p < 1.f || s.min_p > 0.0);
+  return s;
+}
+
+// Workspace, by row and stretch.
+struct SampleWs {
+  float* top;        // largest logit
+  unsigned* usable;  // tokens that can be drawn
+  u64* weight;       // sum of their weights
+  u64* bin_weight;   // [kLogitBins]
+  unsigned short* bin_count;
+  int n;             // stretches per row
+};
 
 __device__ __forceinline__ u64 wave_sum64(u64 v) {
+#pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
   return v;
 }
 
-__global__ void __launch_bounds__(kSampleThreads) k_sample(harli_sample_batch a, double one) {
-  constexpr int NW = kSampleThreads / 64;
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.vocab;
-  const float* z = a.logits + (size_t)b * a.ld;
-  __shared__ float s_max[NW];
-  __shared__ int s_bin, s_first;
-  __shared__ u64 mass[256], s_part[NW], s_above;
-  __shared__ u64 s_ties[NW];
+constexpr int kStretchThreads = 256, kPer = kStretch / kStretchThreads;
 
-  float mx = -INFINITY;
-  for (int i = tid; i < V; i += kSampleThreads) {
-    const float v = z[i];
-    if (v > mx) mx = v;
+__global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample_batch a, SampleWs ws) {
+  __shared__ float s_top[4];
+  __shared__ u64 s_weight[4], bin_weight[kLogitBins];
+  __shared__ unsigned s_n[4], bin_count[kLogitBins];
+  const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, first = blockIdx.x * kStretch;
+  const float* z = a.logits + (size_t)b * a.ld + first;
+  const int n = min(kStretch, a.vocab - first);
+  float v[kPer];
+  if (n == kStretch && (uintptr_t)z % 16 == 0) {  // which thread has which token does not matter here
+#pragma unroll
+    for (int i = 0; i < kPer / 4; ++i) {
+      const float4 x = reinterpret_cast<const float4*>(z)[i * kStretchThreads + tid];
+      v[4 * i] = x.x, v[4 * i + 1] = x.y, v[4 * i + 2] = x.z, v[4 * i + 3] = x.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) v[i] = i * kStretchThreads + tid < n ? z[i * kStretchThreads + tid] : -INFINITY;
   }
-  for (int o = 1; o < 64; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
-  if (lane == 0) s_max[wave] = mx;
-  if (tid == 0) s_first = 0x7fffffff;
+  const RowSettings s = settings_of(a, b);
+  bin_weight[tid] = 0, bin_count[tid] = 0;
+  float top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) top = fmaxf(top, v[i]);  // (NaN is the other operand)
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  if (lane == 0) s_top[wave] = top;
   __syncthreads();
-  for (int w = 0; w < NW; ++w) mx = fmaxf(mx, s_max[w]);
-  if (mx == -INFINITY) {
-    if (tid == 0) {
-      a.token[b] = -1;
-      if (a.logprob) a.logprob[b] = -INFINITY;
-    }
-    return;
-  }
-  const float T = a.temperature ? a.temperature[b] : 1.f;
-  if (!(T > 0.f)) {
-    for (int i = tid; i < V; i += kSampleThreads)
-      if (z[i] == mx) {
-        atomicMin(&s_first, i);
-        break;
+  top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+  const size_t at = (size_t)b * ws.n + blockIdx.x;
+  if (tid == 0) ws.top[at] = top;
+  if (s.greedy) return;
+  const double per_t = 1.4426950408889634074 / (double)s.t;
+  const float per_unit = bins_per_unit(s.t);
+  const int bin0 = bin_of(top, per_unit);
+  u64 sum = 0;
+  unsigned count = 0;
+#pragma unroll 4
+  for (int i = 0; i < kPer; ++i) {
+    if (!usable(v[i])) continue;
+    const u64 w = fixed_of(weight_of(v[i], top, per_t));
+    sum += w;
+    ++count;
+    if (s.cut) {
+      const int bin = bin0 - bin_of(v[i], per_unit);
+      if (bin < kLogitBins) {
+        atomicAdd(&bin_weight[bin], w);
+        if (s.k) atomicAdd(&bin_count[bin], 1u);
       }
-    __syncthreads();
-    if (tid == 0) {
-      a.token[b] = s_first;
-      if (a.logprob) a.logprob[b] = 0.f;
     }
-    return;
   }
-  const double inv_t = 1.0 / (double)T;
-  auto usable = [&](float v) { return v > -INFINITY; };  // (false for NaN)
+  sum = wave_sum64(sum);
+  count = wave_sum(count);
+  if (lane == 0) s_weight[wave] = sum, s_n[wave] = count;
+  __syncthreads();
+  if (tid == 0) {
+    ws.weight[at] = s_weight[0] + s_weight[1] + s_weight[2] + s_weight[3];
+    ws.usable[at] = s_n[0] + s_n[1] + s_n[2] + s_n[3];
+  }
+  if (s.cut) {
+    ws.bin_weight[at * kLogitBins + tid] = bin_weight[tid];
+    if (s.k) ws.bin_count[at * kLogitBins + tid] = (unsigned short)bin_count[tid];
+  }
+}
 
-  // the cut: keys above t_key stay, and the first `ties` of those equal to it
-  unsigned t_key = 0;
-  u64 ties = ~0ull, total = 0;
-  // digit by digit: the key at which what lies above it is less than `want` and with it not; BY_MASS: weights, else tokens
-  auto select = [&](bool by_mass, u64 want, unsigned& key, u64& rest) {
-    unsigned prefix = 0, mask = 0;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) mass[tid] = 0;
-      __syncthreads();
-      for (int i = tid; i < V; i += kSampleThreads) {
-        const float v = z[i];
-        if (!usable(v)) continue;
-        const unsigned k = order_key(v);
-        if ((k & mask) == prefix) atomicAdd(&mass[(k >> shift) & 255], by_mass ? fixed_of(weight_of(v, mx, inv_t), one) : 1ull);
-      }
-      __syncthreads();
-      if (tid == 0) {
-        u64 above = 0;
-        int bin = 255;
-        for (; bin > 0 && above + mass[bin] < want; --bin) above += mass[bin];
-        s_bin = bin, s_above = above;
-      }
-      __syncthreads();
-      want -= s_above;
-      prefix |= (unsigned)s_bin << shift;
-      mask |= 255u << shift;
-      __syncthreads();
-    }
-    key = prefix, rest = want;
-  };
-  // weights above the key, and the number of tokens at it
-  auto sums = [&](unsigned key, u64& above, u64& at) {
-    u64 s = 0, n = 0;
-    for (int i = tid; i < V; i += kSampleThreads) {
-      const float v = z[i];
-      if (!usable(v)) continue;
-      const unsigned k = order_key(v);
-      if (k > key) s += fixed_of(weight_of(v, mx, inv_t), one);
-      else if (k == key) ++n;
-    }
-    s = wave_sum64(s), n = wave_sum64(n);
-    if (lane == 0) s_part[wave] = s, s_ties[wave] = n;
-    __syncthreads();
-    above = at = 0;
-    for (int w = 0; w < NW; ++w) above += s_part[w], at += s_ties[w];
-    __syncthreads();
-  };
-  const int k_row = a.top_k ? a.top_k[b] : 0;
-  const float p_row = a.top_p ? a.top_p[b] : 1.f;
-  double floor_p = a.min_p ? (double)a.min_p[b] : 0.0;
-  floor_p = floor_p > 1.0 ? 1.0 : floor_p > 0.0 ? floor_p : 0.0;
-  u64 above, at;
-  sums(0, above, at);  // (no finite logit and no infinity has key 0)
-  u64 usable_n = 0;
-  if (k_row > 0 && k_row < V) {
-    // fewer usable tokens than k: all of them
-    u64 n = 0;
-    for (int i = tid; i < V; i += kSampleThreads) n += usable(z[i]);
-    n = wave_sum64(n);
-    if (lane == 0) s_part[wave] = n;
-    __syncthreads();
-    for (int w = 0; w < NW; ++w) usable_n += s_part[w];
-    __syncthreads();
-    if ((u64)k_row < usable_n) {
-      select(false, k_row, t_key, ties);
-      sums(t_key, above, at);
-      above += ties * fixed_of(weight_of(order_value(t_key), mx, inv_t), one);
-    }
-  }
-  total = above;
-  if (p_row < 1.f) {
-    const double x = (double)p_row * (double)total;
-    u64 want = x < 1.0 ? 1 : (u64)ceil(x);
-    if (want > total) want = total;
-    unsigned key;
-    u64 rest;
-    select(true, want, key, rest);
-    const u64 w = fixed_of(weight_of(order_value(key), mx, inv_t), one);
-    const u64 n = w ? (rest + w - 1) / w : 1;
-    if (key > t_key || n < ties) t_key = key, ties = n;
-  }
+// ---- the second launch -----------------------------------------------------------------------------------------------------------
+struct RowShared {
+  u64 digit[kDigits];
+  unsigned key[kCandidates], index[kCandidates];
+  float top[kMostStretches];
+  int below[kMostStretches];      // bins from the row's first to the stretch's
+  double scale[kMostStretches];   // weight of the stretch's largest logit in the row
+  double kept[kMostStretches];
+  u64 inside[kMostStretches];     // kept weight of the cut's own bin, in the row's fixed point
+  double bin_weight[kLogitBins];
+  unsigned bin_count[kLogitBins];
+  double part[4][kLogitBins];
+  unsigned part_n[4][kLogitBins];
+  u64 wave64[kRowWaves];
+  double wave_d[kRowWaves];
+  float wave_f[kRowWaves];
+  unsigned wave_u[2 * kRowWaves];
+  u64 found_above;
+  unsigned found;
+  int n;                          // candidates
+};
 
-  // ---- the draw: waves take stretches of the row, by index ---------------------------------------------------------------
-  const int per = ((V + NW - 1) / NW + 63) / 64 * 64, lo = min(V, wave * per), hi = min(V, lo + per);
-  u64 n_at = 0;
-  for (int i = lo + lane; i < hi; i += 64) n_at += usable(z[i]) && order_key(z[i]) == t_key;
-  n_at = wave_sum64(n_at);
-  if (lane == 0) s_ties[wave] = n_at;
+// Sum of v over the threads before this one and over all (whole workgroup).
+__device__ __forceinline__ u64 scan_before64(u64 v, RowShared& sh, int lane, int wave, u64& all) {
+  u64 s = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const u64 x = __shfl_up(s, o, 64);
+    if (lane >= o) s += x;
+  }
+  __syncthreads();
+  if (lane == 63) sh.wave64[wave] = s;
   __syncthreads();
   u64 before = 0;
-  for (int w = 0; w < wave; ++w) before += s_ties[w];
-  auto kept = [&](int i, u64& seen) -> u64 {  // weight of token i (0: not kept); wave collective
-    const float v = i < hi ? z[i] : -INFINITY;
-    const unsigned k = usable(v) ? order_key(v) : 0;
-    const bool tie = usable(v) && k == t_key;
-    const u64 m = __ballot(tie);
-    const u64 r = seen + __popcll(m & ((1ull << lane) - 1));
-    seen += __popcll(m);
-    if (!usable(v) || k < t_key || (tie && r >= ties)) return 0;
-    const double w = weight_of(v, mx, inv_t);
-    return w >= floor_p ? fixed_of(w, one) : 0;
-  };
-  u64 mine = 0, seen = before;
-  for (int i0 = lo; i0 < hi; i0 += 64) mine += kept(i0 + lane, seen);
-  mine = wave_sum64(mine);
-  if (lane == 0) s_part[wave] = mine;
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < kRowWaves; ++w) {
+    if (w < wave) before += sh.wave64[w];
+    all += sh.wave64[w];
+  }
+  return before + s - v;
+}
+
+// The digit, from the highest, at which what the higher ones hold is less than `want` and with it not; sh.digit is filled in.
+// found_above: what the higher ones hold.  want is within the whole.
+__device__ __forceinline__ void find_digit(u64 want, RowShared& sh, int tid, int lane, int wave) {
+  constexpr int BPT = kDigits / kRowThreads;
+  u64 h[BPT], sum = 0, all;
+#pragma unroll
+  for (int i = 0; i < BPT; ++i) h[i] = sh.digit[kDigits - 1 - (tid * BPT + i)], sum += h[i];
+  u64 above = scan_before64(sum, sh, lane, wave, all);
+  if (above < want && above + sum >= want) {
+#pragma unroll
+    for (int i = 0; i < BPT; ++i) {
+      if (above < want && above + h[i] >= want) sh.found = kDigits - 1 - (tid * BPT + i), sh.found_above = above;
+      above += h[i];
+    }
+  }
   __syncthreads();
-  u64 start = 0, all = 0;
-  for (int w = 0; w < NW; ++w) {
-    if (w < wave) start += s_part[w];
-    all += s_part[w];
-  }
-  const float u = a.uniform[b];
-  const double x = u > 0.f ? (double)u * (double)all : 0.0;
-  u64 target = x >= (double)all ? all - 1 : (u64)x;
-  if (target >= all) target = all - 1;
-  if (target < start || target >= start + mine) return;
-  seen = before;
-  for (int i0 = lo; i0 < hi; i0 += 64) {
-    const u64 w = kept(i0 + lane, seen);
-    u64 c = w;
-    for (int o = 1; o < 64; o <<= 1) {
-      const u64 v = __shfl_up(c, o, 64);
-      if (lane >= o) c += v;
+}
+
+// Among n items, key(i) and amount(i) (0: not looked at): the key at which the amounts of higher keys are less than `want` and with its
+// own not; `want` becomes what is missing above it.  Keys differ in the bits below `bits` at most.
+template <typename Key, typename Amount>
+__device__ __forceinline__ unsigned find_key(int n, unsigned common, int bits, Key key, Amount amount, u64& want, RowShared& sh, int tid, int lane, int wave) {
+  unsigned prefix = bits < 32 ? common >> bits << bits : 0;
+  while (bits > 0) {
+    const int width = min(bits, 11), shift = bits - width;
+    for (int i = tid; i < kDigits; i += kRowThreads) sh.digit[i] = 0;
+    __syncthreads();
+    for (int i = tid; i < n; i += kRowThreads) {
+      const u64 w = amount(i);
+      if (!w) continue;
+      const unsigned k = key(i);
+      if (bits == 32 || (k >> bits) == (prefix >> bits)) atomicAdd(&sh.digit[(k >> shift) & ((1u << width) - 1)], w);
     }
-    const u64 hit = __ballot(start + c > target);
-    if (hit) {
-      if (lane == __ffsll(hit) - 1) {
-        a.token[b] = i0 + lane;
-        if (a.logprob) a.logprob[b] = (float)log((double)w / (double)all);
+    __syncthreads();
+    find_digit(want, sh, tid, lane, wave);
+    want -= sh.found_above;
+    prefix |= sh.found << shift;
+    bits = shift;
+    __syncthreads();
+  }
+  return prefix;
+}
+
+__global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a, SampleWs ws) {
+  extern __shared__ __align__(16) char row_lds[];
+  RowShared& sh = *reinterpret_cast<RowShared*>(row_lds);
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.vocab, NS = ws.n;
+  const float* z = a.logits + (size_t)b * a.ld;
+  const size_t at0 = (size_t)b * NS;
+  const RowSettings s = settings_of(a, b);
+
+  // ---- the stretches together ----------------------------------------------------------------------------------------------------
+  auto all_sum = [&](u64 v) {
+    u64 all;
+    (void)scan_before64(v, sh, lane, wave, all);
+    return all;
+  };
+  auto all_sum_d = [&](double v) {  // in a fixed order
+    v = wave_sum(v);
+    __syncthreads();
+    if (lane == 0) sh.wave_d[wave] = v;
+    __syncthreads();
+    v = 0;
+#pragma unroll
+    for (int w = 0; w < kRowWaves; ++w) v += sh.wave_d[w];
+    return v;
+  };
+  const float mine = tid < NS ? ws.top[at0 + tid] : -INFINITY;
+  float top = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  if (lane == 0) sh.wave_f[wave] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kRowWaves; ++w) top = fmaxf(top, sh.wave_f[w]);
+  auto answer = [&](int token, float logprob) {
+    a.token[b] = token;
+    if (a.logprob) a.logprob[b] = logprob;
+  };
+  if (top == -INFINITY) {
+    if (tid == 0) answer(-1, -INFINITY);
+    return;
+  }
+  if (s.greedy) {
+    if (tid == 0) sh.found = 0xffffffffu, sh.n = NS;
+    __syncthreads();
+    if (mine == top) atomicMin(&sh.n, tid);
+    __syncthreads();
+    const int first = sh.n * kStretch;
+    for (int i = first + tid; i < min(V, first + kStretch); i += kRowThreads)
+      if (z[i] == top) atomicMin(&sh.found, (unsigned)i);
+    __syncthreads();
+    if (tid == 0) answer((int)sh.found, 0.f);
+    return;
+  }
+  const double per_t = 1.4426950408889634074 / (double)s.t;
+  const float per_unit = bins_per_unit(s.t);
+  const int bin0 = bin_of(top, per_unit);
+  double whole_mine = 0;
+  if (tid < NS) {
+    sh.top[tid] = mine;
+    sh.below[tid] = usable(mine) ? bin0 - bin_of(mine, per_unit) : kLogitBins;
+    sh.scale[tid] = usable(mine) ? weight_of(mine, top, per_t) : 0.0;
+    whole_mine = (double)ws.weight[at0 + tid] * sh.scale[tid];
+  }
+  double whole = all_sum_d(whole_mine);  // of the row, in the row's fixed point
+  auto row_weight = [&](float v) { return fixed_of(weight_of(v, top, per_t)); };
+  // for sums over a whole row: 2^20 of them fit 62 bits
+  constexpr int kWide = 8;
+  auto wide_weight = [&](float v) { return row_weight(v) >> kWide; };
+
+  // ---- the cut: logits with keys above t_key stay, and of those equal to it the ones up to index last ----------------------------
+  unsigned t_key = 0, last = 0xffffffffu;
+  int held = -1;  // the bin whose tokens are in LDS
+  if (s.cut) {
+    {  // bins of the row
+      const int g = tid & (kLogitBins - 1), grp = tid / kLogitBins;
+      double m = 0;
+      unsigned c = 0;
+#pragma unroll 4
+      for (int i = grp; i < NS; i += kRowThreads / kLogitBins) {
+        const int j = g - sh.below[i];
+        if (j >= 0) {
+          m += (double)ws.bin_weight[(at0 + i) * kLogitBins + j] * sh.scale[i];
+          if (s.k) c += ws.bin_count[(at0 + i) * kLogitBins + j];
+        }
       }
-      return;
+      sh.part[grp][g] = m, sh.part_n[grp][g] = c;
+      __syncthreads();
+      if (tid < kLogitBins) {
+        sh.bin_weight[tid] = (sh.part[0][tid] + sh.part[1][tid]) + (sh.part[2][tid] + sh.part[3][tid]);
+        sh.bin_count[tid] = sh.part_n[0][tid] + sh.part_n[1][tid] + sh.part_n[2][tid] + sh.part_n[3][tid];
+      }
+      __syncthreads();
     }
-    start += __shfl(c, 63, 64);
+    // Tokens of one bin of the row to LDS (their order there is of no account); false: more than fit.  bin: kLogitBins and above: of no bin
+    auto fetch = [&](int bin) {
+      if (bin == held) return sh.n <= kCandidates;
+      __syncthreads();
+      held = bin;
+      if (tid == 0) sh.n = 0;
+      __syncthreads();
+      for (int i = wave; i < NS; i += kRowWaves) {  // a wave per stretch
+        const int j = bin - sh.below[i];
+        if (j < 0 || j >= kLogitBins || bin >= kLogitBins) continue;
+        const bool some = s.k ? ws.bin_count[(at0 + i) * kLogitBins + j] != 0 : ws.bin_weight[(at0 + i) * kLogitBins + j] != 0;
+        if (!some) continue;
+        const int lo = i * kStretch, hi = min(V, lo + kStretch);
+#pragma unroll 8
+        for (int x0 = lo; x0 < hi; x0 += 64) {
+          const int x = x0 + lane;
+          const float v = x < hi ? z[x] : -INFINITY;
+          const bool in = usable(v) && bin0 - bin_of(v, per_unit) == bin;
+          const u64 who = __ballot(in);
+          if (!who) continue;
+          int at = 0;
+          if (lane == 0) at = atomicAdd(&sh.n, (int)__popcll(who));
+          at = __shfl(at, 0, 64) + (int)__popcll(who & ((1ull << lane) - 1));
+          if (in && at < kCandidates) sh.key[at] = order_key(v), sh.index[at] = (unsigned)x;
+        }
+      }
+      __syncthreads();
+      return sh.n <= kCandidates;
+    };
+    // highest differing bit of the candidates' keys
+    auto spread = [&](unsigned& common) {
+      unsigned lo = 0xffffffffu, hi = 0;
+      for (int i = tid; i < sh.n; i += kRowThreads) lo = min(lo, sh.key[i]), hi = max(hi, sh.key[i]);
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) lo = min(lo, (unsigned)__shfl_xor((int)lo, o, 64)), hi = max(hi, (unsigned)__shfl_xor((int)hi, o, 64));
+      __syncthreads();
+      if (lane == 0) sh.wave_u[wave] = lo, sh.wave_u[kRowWaves + wave] = hi;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kRowWaves; ++w) lo = min(lo, sh.wave_u[w]), hi = max(hi, sh.wave_u[kRowWaves + w]);
+      common = hi;
+      return lo == hi ? 0 : 32 - __clz((int)(lo ^ hi));
+    };
+    auto cand_key = [&](int i) { return sh.key[i]; };
+    auto row_key = [&](int i) { return order_key(z[i]); };
+    // of the tokens equal to t_key the first `ties`: the index of the last one
+    u64 ties = ~0ull;
+    double among = whole;
+    if (s.k) {
+      const u64 n_usable = all_sum(tid < NS && usable(mine) ? ws.usable[at0 + tid] : 0);
+      if ((u64)s.k < n_usable) {
+        u64 want = s.k, window = all_sum(tid < kLogitBins ? sh.bin_count[tid] : 0);
+        int bin = kLogitBins;
+        if (want <= window) {
+          u64 all;
+          const u64 before = scan_before64(tid < kLogitBins ? sh.bin_count[tid] : 0, sh, lane, wave, all);
+          if (tid < kLogitBins && before < want && before + sh.bin_count[tid] >= want) sh.found = tid, sh.found_above = before;
+          __syncthreads();
+          bin = sh.found;
+        }
+        if (bin < kLogitBins && fetch(bin)) {
+          want -= sh.found_above;
+          unsigned common;
+          const int bits = spread(common);
+          t_key = find_key(sh.n, common, bits, cand_key, [&](int) { return 1ull; }, want, sh, tid, lane, wave);
+          ties = want;
+          // what the first k weigh
+          u64 w = 0;
+          for (int i = tid; i < sh.n; i += kRowThreads)
+            if (sh.key[i] > t_key) w += row_weight(order_value(sh.key[i]));
+          w = all_sum(w) + ties * row_weight(order_value(t_key));
+          among = all_sum_d(tid < bin ? sh.bin_weight[tid] : 0.0) + (double)w;
+        } else {
+          t_key = find_key(V, 0, 32, row_key, [&](int i) { return usable(z[i]) ? 1ull : 0ull; }, want, sh, tid, lane, wave);
+          ties = want;
+          double w = 0;
+          for (int i = tid; i < V; i += kRowThreads)
+            if (usable(z[i]) && order_key(z[i]) > t_key) w += (double)row_weight(z[i]);
+          among = all_sum_d(w) + (double)ties * (double)row_weight(order_value(t_key));
+        }
+      }
+    }
+    if (s.p < 1.f) {
+      double want = fmax((double)s.p * among, 1.0);  // the first token in any case
+      // weights of the row's bins before each one
+      double v = tid < kLogitBins ? sh.bin_weight[tid] : 0.0, sum = v;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const double x = __shfl_up(sum, o, 64);
+        if (lane >= o) sum += x;
+      }
+      __syncthreads();
+      if (lane == 63) sh.wave_d[wave] = sum;
+      if (tid == 0) sh.found = kLogitBins;
+      __syncthreads();
+      double before = 0;
+      for (int w = 0; w < wave; ++w) before += sh.wave_d[w];
+      const double upto = before + sum;
+      if (tid < kLogitBins && v > 0 && upto >= want) atomicMin(&sh.found, (unsigned)tid);
+      __syncthreads();
+      const int bin = sh.found;
+      if (bin < kLogitBins && tid == bin) sh.wave_d[0] = upto - v;
+      __syncthreads();
+      const double above = sh.wave_d[0];
+      unsigned key;
+      u64 rest;
+      bool by_row = false;
+      if (bin < kLogitBins && fetch(bin)) {
+        unsigned common;
+        const int bits = spread(common);
+        const u64 have = all_sum([&] {
+          u64 w = 0;
+          for (int i = tid; i < sh.n; i += kRowThreads) w += row_weight(order_value(sh.key[i]));
+          return w;
+        }());
+        const double x = ceil(want - above);
+        rest = x < 1.0 ? 1 : x >= (double)have ? have : (u64)x;
+        key = have ? find_key(sh.n, common, bits, cand_key, [&](int i) { return row_weight(order_value(sh.key[i])); }, rest, sh, tid, lane, wave) : 0;
+      } else {
+        by_row = true;
+        const u64 have = all_sum([&] {
+          u64 w = 0;
+          for (int i = tid; i < V; i += kRowThreads)
+            if (usable(z[i])) w += wide_weight(z[i]);
+          return w;
+        }());
+        const double x = ceil(want / (1 << kWide));
+        rest = x >= (double)have ? have : (u64)x;
+        key = find_key(V, 0, 32, row_key, [&](int i) { return usable(z[i]) ? wide_weight(z[i]) : 0ull; }, rest, sh, tid, lane, wave);
+      }
+      if (key) {
+        const u64 w = by_row ? wide_weight(order_value(key)) : row_weight(order_value(key)), n = w ? (rest + w - 1) / w : ~0ull;
+        if (key > t_key) t_key = key, ties = n;
+        else if (key == t_key && n < ties) ties = n;
+      }
+    }
+    if (s.min_p > 0.0) {
+      // the smallest key whose weight is min_p or more: 64 keys at a time, the same search in every wave
+      unsigned lo = 0, hi = order_key(top);  // lo: too small (or 0), hi: large enough
+      while (hi - lo > 1) {
+        const unsigned step = (hi - lo + 63) / 64;
+        const u64 k = (u64)lo + (u64)step * (lane + 1);
+        const bool enough = k >= hi || weight_of(order_value((unsigned)k), top, per_t) >= s.min_p;  // (keys of -NaN weigh nothing)
+        const int i = __ffsll(__ballot(enough)) - 1;  // the last lane is past hi
+        const u64 top_k = (u64)lo + (u64)step * (i + 1);
+        lo += step * i;
+        hi = top_k < hi ? (unsigned)top_k : hi;
+      }
+      if (hi > t_key) t_key = hi, ties = ~0ull;
+    }
+    // the cut's own bin, and the last index of the ties that stay
+    const int bin = t_key ? bin0 - bin_of(order_value(t_key), per_unit) : kLogitBins;
+    const bool in_lds = t_key &&  // the tokens around the cut are candidates (else the row itself is looked through)
+                         bin >= 0 && bin < kLogitBins && fetch(bin);
+    if (t_key) {
+      u64 n_ties = 0;
+      if (in_lds) {
+        for (int i = tid; i < sh.n; i += kRowThreads) n_ties += sh.key[i] == t_key;
+      } else {
+        for (int i = tid; i < V; i += kRowThreads) n_ties += usable(z[i]) && order_key(z[i]) == t_key;
+      }
+      n_ties = all_sum(n_ties);
+      if (ties < n_ties) {
+        u64 want = ties;
+        const unsigned top_index = (unsigned)(kMostVocab - 1);  // smaller indexes first: keys count downwards
+        const unsigned k = in_lds ? find_key(sh.n, 0, 20, [&](int i) { return top_index - sh.index[i]; },
+                                             [&](int i) { return sh.key[i] == t_key ? 1ull : 0ull; }, want, sh, tid, lane, wave)
+                                  : find_key(V, 0, 20, [&](int i) { return top_index - (unsigned)i; },
+                                             [&](int i) { return usable(z[i]) && order_key(z[i]) == t_key ? 1ull : 0ull; }, want, sh, tid, lane, wave);
+        last = top_index - k;
+      }
+    }
+    // kept weight of every stretch
+    if (t_key) {
+      for (int i = tid; i < NS; i += kRowThreads) sh.inside[i] = 0;
+      __syncthreads();
+      if (in_lds) {
+        for (int i = tid; i < sh.n; i += kRowThreads)
+          if (sh.key[i] > t_key || (sh.key[i] == t_key && sh.index[i] <= last)) atomicAdd(&sh.inside[sh.index[i] / kStretch], row_weight(order_value(sh.key[i])));
+        __syncthreads();
+        for (int i = wave; i < NS; i += kRowWaves) {
+          double m = 0;
+#pragma unroll
+          for (int j = 0; j < kLogitBins; j += 64)
+            if (j + lane < bin - sh.below[i]) m += (double)ws.bin_weight[(at0 + i) * kLogitBins + j + lane];
+          m = wave_sum(m);
+          if (lane == 0) sh.kept[i] = m * sh.scale[i] + (double)sh.inside[i];
+        }
+      } else {
+        for (int i = wave; i < NS; i += kRowWaves) {
+          double m = 0;
+          for (int x = i * kStretch + lane; x < min(V, (i + 1) * kStretch); x += 64) {
+            const float v = z[x];
+            if (!usable(v)) continue;
+            const unsigned k = order_key(v);
+            if (k > t_key || (k == t_key && (unsigned)x <= last)) m += (double)row_weight(v);
+          }
+          m = wave_sum(m);
+          if (lane == 0) sh.kept[i] = m;
+        }
+      }
+      __syncthreads();
+    }
   }
+  if (!t_key) {
+    if (tid < NS) sh.kept[tid] = whole_mine;
+    __syncthreads();
+  }
+
+  // ---- the draw ------------------------------------------------------------------------------------------------------------------
+  if (tid == 0) {  // (a sum in the order of the stretches)
+    double all = 0;
+    for (int i = 0; i < NS; ++i) all += sh.kept[i];
+    const float u = a.uniform[b];
+    const double target = u > 0.f ? (double)fminf(u, 1.f) * all : 0.0;
+    double before = 0, start = 0;
+    int pick = 0;
+    for (int i = 0; i < NS; ++i) {
+      if (sh.kept[i] > 0) {
+        pick = i, start = before;
+        if (before + sh.kept[i] > target) break;
+      }
+      before += sh.kept[i];
+    }
+    sh.n = pick;
+    sh.wave_d[0] = all;
+    sh.wave_d[1] = target - start;
+  }
+  __syncthreads();
+  const int pick = sh.n, first = pick * kStretch;
+  const double all = sh.wave_d[0], offset = sh.wave_d[1];
+  const float local = sh.top[pick];
+  u64 w[kStretch / kRowThreads], sum = 0;
+  float v[kStretch / kRowThreads];
+#pragma unroll
+  for (int i = 0; i < kStretch / kRowThreads; ++i) {
+    const int x = first + tid * (kStretch / kRowThreads) + i;
+    v[i] = x < V ? z[x] : -INFINITY;
+    const unsigned k = usable(v[i]) ? order_key(v[i]) : 0;
+    w[i] = usable(v[i]) && (k > t_key || (k == t_key && (unsigned)x <= last)) ? fixed_of(weight_of(v[i], local, per_t)) : 0;
+    sum += w[i];
+  }
+  u64 whole_stretch;
+  u64 before = scan_before64(sum, sh, lane, wave, whole_stretch);
+  const double x = offset / sh.scale[pick];
+  u64 target = x >= (double)whole_stretch ? whole_stretch - 1 : x > 0 ? (u64)x : 0;
+  if (target >= whole_stretch) target = whole_stretch - 1;
+  if (target < before || target >= before + sum) return;
+#pragma unroll
+  for (int i = 0; i < kStretch / kRowThreads; ++i) {
+    if (target >= before && target < before + w[i])
+      answer(first + tid * (kStretch / kRowThreads) + i, (float)log(weight_of(v[i], top, per_t) * kOne / all));
+    before += w[i];
+  }
+}
+
+struct SampleLayout {
+  SampleWs ws;
+  size_t bytes;
+};
+SampleLayout sample_layout(int batch, int vocab, void* base) {
+  auto al = [](size_t n) { return (n + 255) & ~size_t(255); };
+  SampleLayout l{};
+  l.ws.n = (vocab + kStretch - 1) / kStretch;
+  const size_t n = (size_t)batch * l.ws.n;
+  char* p = static_cast<char*>(base);
+  auto take = [&](size_t bytes) {
+    char* q = p + l.bytes;
+    l.bytes += al(bytes);
+    return q;
+  };
+  l.ws.bin_weight = reinterpret_cast<u64*>(take(n * kLogitBins * 8));
+  l.ws.weight = reinterpret_cast<u64*>(take(n * 8));
+  l.ws.top = reinterpret_cast<float*>(take(n * 4));
+  l.ws.usable = reinterpret_cast<unsigned*>(take(n * 4));
+  l.ws.bin_count = reinterpret_cast<unsigned short*>(take(n * kLogitBins * 2));
+  return l;
+}
+
+// k_sample_row needs more dynamic LDS than the default limit; asked for once per device.
+constexpr int kMaxDevices = 64;
+bool g_row_lds[kMaxDevices] = {};
+std::mutex g_row_lds_mu;
+
+harli_status allow_row_lds() {
+  int dev = -1;
+  HARLI_HIP(hipGetDevice(&dev));
+  if (dev < 0 || dev >= kMaxDevices) return fail(HARLI_ERR_INVALID, "sample: device ordinal %d outside 0..%d", dev, kMaxDevices - 1);
+  std::lock_guard<std::mutex> lk(g_row_lds_mu);
+  if (!g_row_lds[dev]) {
+    HARLI_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&k_sample_row), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowShared)));
+    g_row_lds[dev] = true;
+  }
+  return HARLI_OK;
 }
 
 }  // namespace
@@ -214,23 +646,25 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample(harli_sample_batch a,
 using namespace harli;
 
 extern "C" size_t harli_sample_workspace_bytes(int32_t batch, int32_t vocab) {
-  if (batch < 1 || vocab < 1 || vocab > (1 << 24)) return 0;
-  return 256;
+  if (batch < 1 || batch > 65535 || vocab < 1 || vocab > kMostVocab) return 0;
+  return sample_layout(batch, vocab, nullptr).bytes;
 }
 
 extern "C" harli_status harli_sample(const harli_sample_batch* b, void* hip_stream) {
   if (!b) return fail(HARLI_ERR_INVALID, "sample: null argument");
-  if (b->batch < 1) return fail(HARLI_ERR_INVALID, "sample: batch %d", b->batch);
-  if (b->vocab < 1 || b->vocab > (1 << 24)) return fail(HARLI_ERR_INVALID, "sample: vocabulary of %d outside 1..2^24", b->vocab);
+  if (b->batch < 1 || b->batch > 65535) return fail(HARLI_ERR_INVALID, "sample: batch %d outside 1..65535", b->batch);
+  if (b->vocab < 1 || b->vocab > kMostVocab) return fail(HARLI_ERR_INVALID, "sample: vocabulary of %d outside 1..%d", b->vocab, kMostVocab);
   if (!b->logits || !b->uniform || !b->token) return fail(HARLI_ERR_INVALID, "sample: logits, uniform and token are required");
   if (b->ld < b->vocab) return fail(HARLI_ERR_INVALID, "sample: rows %lld apart hold %d logits", (long long)b->ld, b->vocab);
   const size_t need = harli_sample_workspace_bytes(b->batch, b->vocab);
   if (!b->workspace || (uintptr_t)b->workspace % 256 || b->workspace_bytes < need)
     return fail(HARLI_ERR_INVALID, "sample: a 256-byte aligned workspace of %zu bytes is needed, got %zu", need, b->workspace ? b->workspace_bytes : 0);
-  int bits = 0;
-  while ((1ll << bits) < b->vocab) ++bits;
-  const double one = (double)(1ull << (62 - bits));
-  hipLaunchKernelGGL(k_sample, dim3(b->batch), dim3(kSampleThreads), 0, static_cast<hipStream_t>(hip_stream), *b, one);
+  harli_status rc = allow_row_lds();
+  if (rc != HARLI_OK) return rc;
+  const SampleWs ws = sample_layout(b->batch, b->vocab, b->workspace).ws;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  hipLaunchKernelGGL(k_sample_stretch, dim3(ws.n, b->batch), dim3(kStretchThreads), 0, st, *b, ws);
+  hipLaunchKernelGGL(k_sample_row, dim3(b->batch), dim3(kRowThreads), sizeof(RowShared), st, *b, ws);
   HARLI_HIP(hipGetLastError());
   return HARLI_OK;
 }

@@ -67,8 +67,9 @@ def test_sample_refuses_bad_arguments_on_the_host():
         return ctypes.byref(hb.SampleBatch(**dict(good, **kw))), None
 
     refused("null", l.harli_sample, None, None)
-    refused("batch", l.harli_sample, *call(batch=0))
-    for v in (0, -1, (1 << 24) + 1):
+    for n in (0, 65536):
+        refused("batch", l.harli_sample, *call(batch=n))
+    for v in (0, -1, (1 << 20) + 1):
         refused("vocabulary", l.harli_sample, *call(vocab=v))
         assert hb.sample_workspace_bytes(2, v) == 0
     for name in ("logits", "uniform", "token"):
