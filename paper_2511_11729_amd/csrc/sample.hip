@@ -26,7 +26,7 @@ constexpr int kMostStretches = kMostVocab / kStretch;
 constexpr int kLogitBins = 256;     // of a stretch, downwards from its maximum
 constexpr int kCandidates = 8192;   // tokens of one bin that the second launch holds in LDS
 constexpr int kDigits = 2048;       // bins of a search: 11 bits
-constexpr int kRowThreads = 1024, kRowWaves = kRowThreads / 64;
+constexpr int kRowThreads = 512, kRowWaves = kRowThreads / 64;
 constexpr double kOne = (double)(1ull << 50);  // weight 1 in fixed point: 2^12 of them and more fit 64 bits
 
 // Order of the logits as unsigned integers; both zeros alike.
@@ -37,21 +37,36 @@ __device__ __forceinline__ unsigned order_key(float v) {
 __device__ __forceinline__ float order_value(unsigned k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 __device__ __forceinline__ bool usable(float v) { return v > -INFINITY; }  // (not NaN either)
 
-// 2^t for t <= 0: t = n + f, the series of 2^f = exp(f ln 2) over |f| <= 1/2 to the eleventh power (what follows is below 7e-15)
-__device__ __forceinline__ double exp2_series(double t) {
-  constexpr double l = 0.693147180559945309417;
-  constexpr double c1 = l, c2 = c1 * l / 2, c3 = c2 * l / 3, c4 = c3 * l / 4, c5 = c4 * l / 5, c6 = c5 * l / 6, c7 = c6 * l / 7, c8 = c7 * l / 8,
-                   c9 = c8 * l / 9, c10 = c9 * l / 10, c11 = c10 * l / 11;
-  t = fmax(t, -1080.0);  // zero in any case
-  const double n = rint(t), f = t - n;
-  double p = c11;
-  p = fma(p, f, c10), p = fma(p, f, c9), p = fma(p, f, c8), p = fma(p, f, c7), p = fma(p, f, c6), p = fma(p, f, c5), p = fma(p, f, c4);
-  p = fma(p, f, c3), p = fma(p, f, c2), p = fma(p, f, c1), p = fma(p, f, 1.0);
-  return __builtin_amdgcn_ldexp(p, (int)n);
+// 2^(j / 32), by the series of exp (constant expressions: the compiler's own doubles)
+constexpr double exp_series(double x) {
+  double sum = 1, term = 1;
+  for (int i = 1; i < 24; ++i) term = term * x / i, sum += term;
+  return sum;
 }
-// weight of a usable logit, relative to `top`; per_t = log2(e) / temperature
-__device__ __forceinline__ double weight_of(float v, float top, double per_t) {
-  return v == top ? 1.0 : top == INFINITY || v == -INFINITY ? 0.0 : exp2_series(((double)v - (double)top) * per_t);
+constexpr double kLn2 = 0.693147180559945309417;
+struct PowerTable {
+  double v[32];
+};
+constexpr PowerTable make_powers() {
+  PowerTable t{};
+  for (int j = 0; j < 32; ++j) t.v[j] = exp_series(kLn2 * j / 32);
+  return t;
+}
+__constant__ PowerTable kPowers = make_powers();
+
+// 2^(t / 32): t = 32 e + j + f; the table's 2^(j / 32) times the series of exp(f ln 2 / 32) over |f| <= 1/2 to the fifth power (what
+// follows is below 3e-15).  `powers`: the table in LDS, where its 32 entries lie in banks of their own.
+__device__ __forceinline__ double exp2_32nds(double t, const double* powers) {
+  constexpr double l = kLn2 / 32, c1 = l, c2 = c1 * l / 2, c3 = c2 * l / 3, c4 = c3 * l / 4, c5 = c4 * l / 5;
+  const double n = rint(t), f = t - n;
+  const int i = (int)n;  // (far below the range it saturates: zero)
+  const double p = fma(fma(fma(fma(fma(c5, f, c4), f, c3), f, c2), f, c1), f, 1.0);
+  return __builtin_amdgcn_ldexp(p * powers[i & 31], i >> 5);
+}
+// weight of a usable logit relative to `top`; per_t = 32 log2(e) / temperature
+__device__ __forceinline__ double weight_of(float v, float top, double per_t, const double* powers) {
+  if (top == INFINITY) return v == top ? 1.0 : 0.0;
+  return exp2_32nds(((double)v - (double)top) * per_t, powers);
 }
 __device__ __forceinline__ u64 fixed_of(double w) {  // w <= 1: added to 2^52, its integer part stands in the low bits, rounded
   return (u64)__double_as_longlong(fma(w, kOne, (double)(1ull << 52))) & ((1ull << 52) - 1);
@@ -64,6 +79,7 @@ __device__ __forceinline__ int bin_of(float v, float per_unit) {  // monotone; k
   return (int)floorf(fminf(fmaxf(v * per_unit, -5e8f), 5e8f));
 }
 
+constexpr double kPerT = 32 * 1.4426950408889634074;
 struct RowSettings {
   float t, p;
   double min_p;
@@ -105,6 +121,7 @@ constexpr int kStretchThreads = 256, kPer = kStretch / kStretchThreads;
 __global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample_batch a, SampleWs ws) {
   __shared__ float s_top[4];
   __shared__ u64 s_weight[4], bin_weight[kLogitBins];
+  __shared__ double powers[32];
   __shared__ unsigned s_n[4], bin_count[kLogitBins];
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, first = blockIdx.x * kStretch;
   const float* z = a.logits + (size_t)b * a.ld + first;
@@ -122,6 +139,7 @@ __global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample
   }
   const RowSettings s = settings_of(a, b);
   bin_weight[tid] = 0, bin_count[tid] = 0;
+  if (tid < 32) powers[tid] = kPowers.v[tid];
   float top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) top = fmaxf(top, v[i]);  // (NaN is the other operand)
@@ -133,21 +151,21 @@ __global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample
   const size_t at = (size_t)b * ws.n + blockIdx.x;
   if (tid == 0) ws.top[at] = top;
   if (s.greedy) return;
-  const double per_t = 1.4426950408889634074 / (double)s.t;
+  const double per_t = kPerT / (double)s.t;
   const float per_unit = bins_per_unit(s.t);
   const int bin0 = bin_of(top, per_unit);
   u64 sum = 0;
   unsigned count = 0;
 #pragma unroll 4
   for (int i = 0; i < kPer; ++i) {
-    if (!usable(v[i])) continue;
-    const u64 w = fixed_of(weight_of(v[i], top, per_t));
+    const bool in = usable(v[i]);
+    const u64 w = in ? fixed_of(weight_of(v[i], top, per_t, powers)) : 0;
     sum += w;
-    ++count;
+    count += in;
     if (s.cut) {
       const int bin = bin0 - bin_of(v[i], per_unit);
-      if (bin < kLogitBins) {
-        atomicAdd(&bin_weight[bin], w);
+      if (in && bin < kLogitBins) {
+        if (w) atomicAdd(&bin_weight[bin], w);
         if (s.k) atomicAdd(&bin_count[bin], 1u);
       }
     }
@@ -167,8 +185,11 @@ __global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample
 }
 
 // ---- the second launch -----------------------------------------------------------------------------------------------------------
+// Its steps are short and depend on one another, so what it costs is their latency, and its own code: a launch finds the instruction cache
+// cold.  The three searches (for top-k, for top-p, for the last of equal logits) are therefore one loop around one search.
 struct RowShared {
   u64 digit[kDigits];
+  double powers[32];
   unsigned key[kCandidates], index[kCandidates];
   float top[kMostStretches];
   int below[kMostStretches];      // bins from the row's first to the stretch's
@@ -177,13 +198,14 @@ struct RowShared {
   u64 inside[kMostStretches];     // kept weight of the cut's own bin, in the row's fixed point
   double bin_weight[kLogitBins];
   unsigned bin_count[kLogitBins];
-  double part[4][kLogitBins];
-  unsigned part_n[4][kLogitBins];
+  double part[kRowThreads / kLogitBins][kLogitBins];
+  unsigned part_n[kRowThreads / kLogitBins][kLogitBins];
   u64 wave64[kRowWaves];
   double wave_d[kRowWaves];
   float wave_f[kRowWaves];
   unsigned wave_u[2 * kRowWaves];
   u64 found_above;
+  double found_above_d;
   unsigned found;
   int n;                          // candidates
 };
@@ -208,6 +230,26 @@ __device__ __forceinline__ u64 scan_before64(u64 v, RowShared& sh, int lane, int
   }
   return before + s - v;
 }
+__device__ __forceinline__ u64 all_sum(u64 v, RowShared& sh, int lane, int wave) {
+  v = wave_sum64(v);
+  __syncthreads();
+  if (lane == 0) sh.wave64[wave] = v;
+  __syncthreads();
+  v = 0;
+#pragma unroll
+  for (int w = 0; w < kRowWaves; ++w) v += sh.wave64[w];
+  return v;
+}
+__device__ __forceinline__ double all_sum(double v, RowShared& sh, int lane, int wave) {  // in a fixed order
+  v = wave_sum(v);
+  __syncthreads();
+  if (lane == 0) sh.wave_d[wave] = v;
+  __syncthreads();
+  v = 0;
+#pragma unroll
+  for (int w = 0; w < kRowWaves; ++w) v += sh.wave_d[w];
+  return v;
+}
 
 // The digit, from the highest, at which what the higher ones hold is less than `want` and with it not; sh.digit is filled in.
 // found_above: what the higher ones hold.  want is within the whole.
@@ -228,26 +270,28 @@ __device__ __forceinline__ void find_digit(u64 want, RowShared& sh, int tid, int
 }
 
 // Among n items, key(i) and amount(i) (0: not looked at): the key at which the amounts of higher keys are less than `want` and with its
-// own not; `want` becomes what is missing above it.  Keys differ in the bits below `bits` at most.
+// own not; `want` becomes what is missing above it.  Keys agree with `common` from bit `bits` on.
 template <typename Key, typename Amount>
 __device__ __forceinline__ unsigned find_key(int n, unsigned common, int bits, Key key, Amount amount, u64& want, RowShared& sh, int tid, int lane, int wave) {
   unsigned prefix = bits < 32 ? common >> bits << bits : 0;
+#pragma unroll 1
   while (bits > 0) {
     const int width = min(bits, 11), shift = bits - width;
     for (int i = tid; i < kDigits; i += kRowThreads) sh.digit[i] = 0;
     __syncthreads();
+#pragma unroll 1
     for (int i = tid; i < n; i += kRowThreads) {
-      const u64 w = amount(i);
-      if (!w) continue;
       const unsigned k = key(i);
-      if (bits == 32 || (k >> bits) == (prefix >> bits)) atomicAdd(&sh.digit[(k >> shift) & ((1u << width) - 1)], w);
+      if (bits == 32 || (k >> bits) == (prefix >> bits)) {
+        const u64 w = amount(i);
+        if (w) atomicAdd(&sh.digit[(k >> shift) & ((1u << width) - 1)], w);
+      }
     }
     __syncthreads();
     find_digit(want, sh, tid, lane, wave);
     want -= sh.found_above;
     prefix |= sh.found << shift;
     bits = shift;
-    __syncthreads();
   }
   return prefix;
 }
@@ -255,32 +299,19 @@ __device__ __forceinline__ unsigned find_key(int n, unsigned common, int bits, K
 __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a, SampleWs ws) {
   extern __shared__ __align__(16) char row_lds[];
   RowShared& sh = *reinterpret_cast<RowShared*>(row_lds);
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.vocab, NS = ws.n;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = a.vocab, NS = ws.n;
   const float* z = a.logits + (size_t)b * a.ld;
   const size_t at0 = (size_t)b * NS;
   const RowSettings s = settings_of(a, b);
 
   // ---- the stretches together ----------------------------------------------------------------------------------------------------
-  auto all_sum = [&](u64 v) {
-    u64 all;
-    (void)scan_before64(v, sh, lane, wave, all);
-    return all;
-  };
-  auto all_sum_d = [&](double v) {  // in a fixed order
-    v = wave_sum(v);
-    __syncthreads();
-    if (lane == 0) sh.wave_d[wave] = v;
-    __syncthreads();
-    v = 0;
-#pragma unroll
-    for (int w = 0; w < kRowWaves; ++w) v += sh.wave_d[w];
-    return v;
-  };
   const float mine = tid < NS ? ws.top[at0 + tid] : -INFINITY;
   float top = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
   if (lane == 0) sh.wave_f[wave] = top;
+  if (tid < 32) sh.powers[tid] = kPowers.v[tid];
+  if (tid == 0) sh.found = 0xffffffffu, sh.n = NS;
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kRowWaves; ++w) top = fmaxf(top, sh.wave_f[w]);
@@ -293,8 +324,6 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
     return;
   }
   if (s.greedy) {
-    if (tid == 0) sh.found = 0xffffffffu, sh.n = NS;
-    __syncthreads();
     if (mine == top) atomicMin(&sh.n, tid);
     __syncthreads();
     const int first = sh.n * kStretch;
@@ -304,26 +333,24 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
     if (tid == 0) answer((int)sh.found, 0.f);
     return;
   }
-  const double per_t = 1.4426950408889634074 / (double)s.t;
+  const double per_t = kPerT / (double)s.t;
+  const double* powers = sh.powers;
   const float per_unit = bins_per_unit(s.t);
   const int bin0 = bin_of(top, per_unit);
   double whole_mine = 0;
   if (tid < NS) {
     sh.top[tid] = mine;
     sh.below[tid] = usable(mine) ? bin0 - bin_of(mine, per_unit) : kLogitBins;
-    sh.scale[tid] = usable(mine) ? weight_of(mine, top, per_t) : 0.0;
+    sh.scale[tid] = usable(mine) ? weight_of(mine, top, per_t, powers) : 0.0;
     whole_mine = (double)ws.weight[at0 + tid] * sh.scale[tid];
+    sh.kept[tid] = whole_mine;
   }
-  double whole = all_sum_d(whole_mine);  // of the row, in the row's fixed point
-  auto row_weight = [&](float v) { return fixed_of(weight_of(v, top, per_t)); };
-  // for sums over a whole row: 2^20 of them fit 62 bits
-  constexpr int kWide = 8;
-  auto wide_weight = [&](float v) { return row_weight(v) >> kWide; };
+  auto row_weight = [&](unsigned key) { return fixed_of(weight_of(order_value(key), top, per_t, powers)); };
 
   // ---- the cut: logits with keys above t_key stay, and of those equal to it the ones up to index last ----------------------------
   unsigned t_key = 0, last = 0xffffffffu;
-  int held = -1;  // the bin whose tokens are in LDS
   if (s.cut) {
+    double among = all_sum(whole_mine, sh, lane, wave);  // weight of the tokens that top-k leaves, in the row's fixed point
     {  // bins of the row
       const int g = tid & (kLogitBins - 1), grp = tid / kLogitBins;
       double m = 0;
@@ -339,190 +366,196 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
       sh.part[grp][g] = m, sh.part_n[grp][g] = c;
       __syncthreads();
       if (tid < kLogitBins) {
-        sh.bin_weight[tid] = (sh.part[0][tid] + sh.part[1][tid]) + (sh.part[2][tid] + sh.part[3][tid]);
-        sh.bin_count[tid] = sh.part_n[0][tid] + sh.part_n[1][tid] + sh.part_n[2][tid] + sh.part_n[3][tid];
-      }
-      __syncthreads();
-    }
-    // Tokens of one bin of the row to LDS (their order there is of no account); false: more than fit.  bin: kLogitBins and above: of no bin
-    auto fetch = [&](int bin) {
-      if (bin == held) return sh.n <= kCandidates;
-      __syncthreads();
-      held = bin;
-      if (tid == 0) sh.n = 0;
-      __syncthreads();
-      for (int i = wave; i < NS; i += kRowWaves) {  // a wave per stretch
-        const int j = bin - sh.below[i];
-        if (j < 0 || j >= kLogitBins || bin >= kLogitBins) continue;
-        const bool some = s.k ? ws.bin_count[(at0 + i) * kLogitBins + j] != 0 : ws.bin_weight[(at0 + i) * kLogitBins + j] != 0;
-        if (!some) continue;
-        const int lo = i * kStretch, hi = min(V, lo + kStretch);
-#pragma unroll 8
-        for (int x0 = lo; x0 < hi; x0 += 64) {
-          const int x = x0 + lane;
-          const float v = x < hi ? z[x] : -INFINITY;
-          const bool in = usable(v) && bin0 - bin_of(v, per_unit) == bin;
-          const u64 who = __ballot(in);
-          if (!who) continue;
-          int at = 0;
-          if (lane == 0) at = atomicAdd(&sh.n, (int)__popcll(who));
-          at = __shfl(at, 0, 64) + (int)__popcll(who & ((1ull << lane) - 1));
-          if (in && at < kCandidates) sh.key[at] = order_key(v), sh.index[at] = (unsigned)x;
-        }
-      }
-      __syncthreads();
-      return sh.n <= kCandidates;
-    };
-    // highest differing bit of the candidates' keys
-    auto spread = [&](unsigned& common) {
-      unsigned lo = 0xffffffffu, hi = 0;
-      for (int i = tid; i < sh.n; i += kRowThreads) lo = min(lo, sh.key[i]), hi = max(hi, sh.key[i]);
+        m = 0, c = 0;
 #pragma unroll
-      for (int o = 1; o < 64; o <<= 1) lo = min(lo, (unsigned)__shfl_xor((int)lo, o, 64)), hi = max(hi, (unsigned)__shfl_xor((int)hi, o, 64));
-      __syncthreads();
-      if (lane == 0) sh.wave_u[wave] = lo, sh.wave_u[kRowWaves + wave] = hi;
-      __syncthreads();
-#pragma unroll
-      for (int w = 0; w < kRowWaves; ++w) lo = min(lo, sh.wave_u[w]), hi = max(hi, sh.wave_u[kRowWaves + w]);
-      common = hi;
-      return lo == hi ? 0 : 32 - __clz((int)(lo ^ hi));
-    };
-    auto cand_key = [&](int i) { return sh.key[i]; };
-    auto row_key = [&](int i) { return order_key(z[i]); };
-    // of the tokens equal to t_key the first `ties`: the index of the last one
-    u64 ties = ~0ull;
-    double among = whole;
-    if (s.k) {
-      const u64 n_usable = all_sum(tid < NS && usable(mine) ? ws.usable[at0 + tid] : 0);
-      if ((u64)s.k < n_usable) {
-        u64 want = s.k, window = all_sum(tid < kLogitBins ? sh.bin_count[tid] : 0);
-        int bin = kLogitBins;
-        if (want <= window) {
-          u64 all;
-          const u64 before = scan_before64(tid < kLogitBins ? sh.bin_count[tid] : 0, sh, lane, wave, all);
-          if (tid < kLogitBins && before < want && before + sh.bin_count[tid] >= want) sh.found = tid, sh.found_above = before;
-          __syncthreads();
-          bin = sh.found;
-        }
-        if (bin < kLogitBins && fetch(bin)) {
-          want -= sh.found_above;
-          unsigned common;
-          const int bits = spread(common);
-          t_key = find_key(sh.n, common, bits, cand_key, [&](int) { return 1ull; }, want, sh, tid, lane, wave);
-          ties = want;
-          // what the first k weigh
-          u64 w = 0;
-          for (int i = tid; i < sh.n; i += kRowThreads)
-            if (sh.key[i] > t_key) w += row_weight(order_value(sh.key[i]));
-          w = all_sum(w) + ties * row_weight(order_value(t_key));
-          among = all_sum_d(tid < bin ? sh.bin_weight[tid] : 0.0) + (double)w;
-        } else {
-          t_key = find_key(V, 0, 32, row_key, [&](int i) { return usable(z[i]) ? 1ull : 0ull; }, want, sh, tid, lane, wave);
-          ties = want;
-          double w = 0;
-          for (int i = tid; i < V; i += kRowThreads)
-            if (usable(z[i]) && order_key(z[i]) > t_key) w += (double)row_weight(z[i]);
-          among = all_sum_d(w) + (double)ties * (double)row_weight(order_value(t_key));
-        }
+        for (int x = 0; x < kRowThreads / kLogitBins; ++x) m += sh.part[x][tid], c += sh.part_n[x][tid];
+        sh.bin_weight[tid] = m, sh.bin_count[tid] = c;
       }
     }
-    if (s.p < 1.f) {
-      double want = fmax((double)s.p * among, 1.0);  // the first token in any case
-      // weights of the row's bins before each one
-      double v = tid < kLogitBins ? sh.bin_weight[tid] : 0.0, sum = v;
+    u64 ties = ~0ull;  // how many of the tokens equal to t_key stay
+    int held = -1;     // the bin whose tokens are in LDS
+    bool in_lds = false;
+#pragma unroll 1
+    for (int phase = 0; phase < 3; ++phase) {
+      int bin = kLogitBins;  // that the phase looks into; kLogitBins: none of them, it looks through the row
+      u64 want = 0;
+      double want_d = 0;
+      if (phase == 0) {  // top-k
+        if (!s.k) continue;
+        if ((u64)s.k >= all_sum((u64)(tid < NS && usable(mine) ? ws.usable[at0 + tid] : 0), sh, lane, wave)) continue;  // (as many as there are)
+        want = s.k;
+        u64 all;
+        const u64 n = tid < kLogitBins ? sh.bin_count[tid] : 0, before = scan_before64(n, sh, lane, wave, all);
+        if (before < want && before + n >= want) sh.found = tid, sh.found_above = before;
+        __syncthreads();
+        if (want <= all) bin = sh.found;
+      } else if (phase == 1) {  // top-p
+        if (!(s.p < 1.f)) continue;
+        want_d = fmax((double)s.p * among, 1.0);  // (the first token in any case)
+        __syncthreads();
+        const double v = tid < kLogitBins ? sh.bin_weight[tid] : 0.0;
+        double upto = v;
 #pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const double x = __shfl_up(sum, o, 64);
-        if (lane >= o) sum += x;
+        for (int o = 1; o < 64; o <<= 1) {
+          const double x = __shfl_up(upto, o, 64);
+          if (lane >= o) upto += x;
+        }
+        if (lane == 63) sh.wave_d[wave] = upto;
+        if (tid == 0) sh.found = kLogitBins;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) upto += sh.wave_d[w];
+        if (v > 0 && upto >= want_d) atomicMin(&sh.found, (unsigned)tid);
+        __syncthreads();
+        bin = sh.found;
+        if (tid == bin) sh.found_above_d = upto - v;
+      } else {  // the cut's own bin, for the last of equal logits and for the weights
+        if (s.min_p > 0.0) {
+          // the smallest key whose weight is min_p or more: 64 keys at a time, the same search in every wave
+          unsigned lo = 0, hi = order_key(top);  // lo: too small, hi: large enough
+#pragma unroll 1
+          while (hi - lo > 1) {
+            const unsigned step = (hi - lo + 63) / 64;
+            const u64 k = (u64)lo + (u64)step * (lane + 1);
+            const bool enough = k >= hi || weight_of(order_value((unsigned)k), top, per_t, powers) >= s.min_p;  // (keys of NaN weigh nothing)
+            const int i = __ffsll(__ballot(enough)) - 1;  // the last lane is past hi
+            const u64 next = (u64)lo + (u64)step * (i + 1);
+            lo += step * i;
+            hi = next < hi ? (unsigned)next : hi;
+          }
+          if (hi > t_key) t_key = hi, ties = ~0ull;
+        }
+        if (!t_key) break;
+        bin = bin0 - bin_of(order_value(t_key), per_unit);
       }
-      __syncthreads();
-      if (lane == 63) sh.wave_d[wave] = sum;
-      if (tid == 0) sh.found = kLogitBins;
-      __syncthreads();
-      double before = 0;
-      for (int w = 0; w < wave; ++w) before += sh.wave_d[w];
-      const double upto = before + sum;
-      if (tid < kLogitBins && v > 0 && upto >= want) atomicMin(&sh.found, (unsigned)tid);
-      __syncthreads();
-      const int bin = sh.found;
-      if (bin < kLogitBins && tid == bin) sh.wave_d[0] = upto - v;
-      __syncthreads();
-      const double above = sh.wave_d[0];
-      unsigned key;
-      u64 rest;
-      bool by_row = false;
-      if (bin < kLogitBins && fetch(bin)) {
-        unsigned common;
-        const int bits = spread(common);
-        const u64 have = all_sum([&] {
-          u64 w = 0;
-          for (int i = tid; i < sh.n; i += kRowThreads) w += row_weight(order_value(sh.key[i]));
-          return w;
-        }());
-        const double x = ceil(want - above);
-        rest = x < 1.0 ? 1 : x >= (double)have ? have : (u64)x;
-        key = have ? find_key(sh.n, common, bits, cand_key, [&](int i) { return row_weight(order_value(sh.key[i])); }, rest, sh, tid, lane, wave) : 0;
+
+      // ---- the tokens of the bin, in LDS (their order there is of no account)
+      if (bin < kLogitBins && bin != held) {
+        __syncthreads();
+        held = bin;
+        if (tid == 0) sh.n = 0;
+        __syncthreads();
+#pragma unroll 1
+        for (int i = wave; i < NS; i += kRowWaves) {  // a wave per stretch
+          const int j = bin - sh.below[i];
+          if (j < 0) continue;
+          const size_t e = (at0 + i) * kLogitBins + j;
+          if (s.k ? ws.bin_count[e] == 0 : ws.bin_weight[e] == 0) continue;
+          // all of the stretch in flight, then a bit per token, then their places with one addition to the common count
+          constexpr int R = kStretch / 64;
+          const int lo = i * kStretch, hi = min(V, lo + kStretch);
+          const bool wide = hi - lo == kStretch && (uintptr_t)(z + lo) % 16 == 0;
+          float v[R];
+          if (wide) {
+#pragma unroll
+            for (int r = 0; r < R / 4; ++r) {
+              const float4 x = reinterpret_cast<const float4*>(z + lo)[r * 64 + lane];
+              v[4 * r] = x.x, v[4 * r + 1] = x.y, v[4 * r + 2] = x.z, v[4 * r + 3] = x.w;
+            }
+          } else {
+#pragma unroll
+            for (int r = 0; r < R; ++r) v[r] = z[min(lo + r * 64 + lane, hi - 1)];
+          }
+          const int target = bin0 - bin, first = wide ? lane * 4 : lane;
+          u64 in = 0;
+#pragma unroll
+          for (int r = 0; r < R; ++r) in |= (u64)(usable(v[r]) && bin_of(v[r], per_unit) == target) << r;
+          if (!wide) {  // what lies behind the row repeated its last token
+            const int n = lo + lane < hi ? (hi - lo - lane + 63) / 64 : 0;
+            if (n < 64) in &= (1ull << n) - 1;
+          }
+          const int mine_n = __popcll(in);
+          int at = mine_n;
+#pragma unroll
+          for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(at, o, 64);
+            if (lane >= o) at += x;
+          }
+          int base = 0;
+          if (lane == 63) base = atomicAdd(&sh.n, at);
+          at += __shfl(base, 63, 64) - mine_n;
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            if (in >> r & 1) {
+              if (at < kCandidates) sh.key[at] = order_key(v[r]), sh.index[at] = (unsigned)(lo + first + (wide ? (r >> 2) * 256 + (r & 3) : r * 64));
+              ++at;
+            }
+        }
+        __syncthreads();
+      }
+      in_lds = bin < kLogitBins && sh.n <= kCandidates;
+      const int n = in_lds ? sh.n : V;
+      // what the search looks at: the candidates, or all of the row
+      auto key_at = [&](int i) { return in_lds ? sh.key[i] : usable(z[i]) ? order_key(z[i]) : 0u; };
+      const int wide_sum = in_lds ? 0 : 8;  // sums over a whole row: 2^20 weights fit 62 bits
+      unsigned common = 0;
+      int bits = 32;
+      if (phase == 2) {
+        u64 equal = 0;
+        for (int i = tid; i < n; i += kRowThreads) equal += key_at(i) == t_key;
+        if (ties >= all_sum(equal, sh, lane, wave)) break;  // all of them
+        want = ties;
+        bits = 20;
+      } else if (in_lds) {  // the highest bit in which the candidates differ
+        unsigned lo = 0xffffffffu, hi = 0;
+        for (int i = tid; i < n; i += kRowThreads) lo = min(lo, sh.key[i]), hi = max(hi, sh.key[i]);
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) lo = min(lo, (unsigned)__shfl_xor((int)lo, o, 64)), hi = max(hi, (unsigned)__shfl_xor((int)hi, o, 64));
+        if (lane == 0) sh.wave_u[wave] = lo, sh.wave_u[kRowWaves + wave] = hi;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kRowWaves; ++w) lo = min(lo, sh.wave_u[w]), hi = max(hi, sh.wave_u[kRowWaves + w]);
+        common = hi;
+        bits = lo == hi ? 0 : 32 - __clz((int)(lo ^ hi));
+      }
+      if (phase == 0 && in_lds) want -= sh.found_above;
+      if (phase == 1) {
+        u64 have = 0;
+        for (int i = tid; i < n; i += kRowThreads) {
+          const unsigned k = key_at(i);
+          if (k) have += row_weight(k) >> wide_sum;
+        }
+        have = all_sum(have, sh, lane, wave);
+        const double x = in_lds ? ceil(want_d - sh.found_above_d) : ceil(want_d / 256);
+        want = x < 1.0 ? 1 : x >= (double)have ? have : (u64)x;
+        if (have == 0) continue;  // (weights that round to nothing: they are not drawn anyway)
+      }
+      const unsigned key = find_key(
+          n, common, bits, [&](int i) { return phase == 2 ? (unsigned)(kMostVocab - 1) - (in_lds ? sh.index[i] : (unsigned)i) : key_at(i); },
+          [&](int i) -> u64 {
+            const unsigned k = key_at(i);
+            return phase == 2 ? k == t_key : k == 0 ? 0 : phase == 0 ? 1 : row_weight(k) >> wide_sum;
+          },
+          want, sh, tid, lane, wave);
+      if (phase == 0) {
+        t_key = key, ties = want;
+        double w = 0;  // what the first k weigh: above the bin, and the candidates above the cut (or the row's tokens above it)
+        u64 w64 = 0;
+        for (int i = tid; i < n; i += kRowThreads) {
+          const unsigned k = key_at(i);
+          if (k > key) {
+            if (in_lds) w64 += row_weight(k);
+            else w += (double)row_weight(k);
+          }
+        }
+        if (in_lds) w = (double)w64 + (tid < bin ? sh.bin_weight[tid] : 0.0);
+        among = all_sum(w, sh, lane, wave) + (double)ties * (double)row_weight(key);
+      } else if (phase == 1) {
+        const u64 w = row_weight(key) >> wide_sum, of_key = w ? (want + w - 1) / w : ~0ull;
+        if (key > t_key) t_key = key, ties = of_key;
+        else if (key == t_key && of_key < ties) ties = of_key;
       } else {
-        by_row = true;
-        const u64 have = all_sum([&] {
-          u64 w = 0;
-          for (int i = tid; i < V; i += kRowThreads)
-            if (usable(z[i])) w += wide_weight(z[i]);
-          return w;
-        }());
-        const double x = ceil(want / (1 << kWide));
-        rest = x >= (double)have ? have : (u64)x;
-        key = find_key(V, 0, 32, row_key, [&](int i) { return usable(z[i]) ? wide_weight(z[i]) : 0ull; }, rest, sh, tid, lane, wave);
-      }
-      if (key) {
-        const u64 w = by_row ? wide_weight(order_value(key)) : row_weight(order_value(key)), n = w ? (rest + w - 1) / w : ~0ull;
-        if (key > t_key) t_key = key, ties = n;
-        else if (key == t_key && n < ties) ties = n;
-      }
-    }
-    if (s.min_p > 0.0) {
-      // the smallest key whose weight is min_p or more: 64 keys at a time, the same search in every wave
-      unsigned lo = 0, hi = order_key(top);  // lo: too small (or 0), hi: large enough
-      while (hi - lo > 1) {
-        const unsigned step = (hi - lo + 63) / 64;
-        const u64 k = (u64)lo + (u64)step * (lane + 1);
-        const bool enough = k >= hi || weight_of(order_value((unsigned)k), top, per_t) >= s.min_p;  // (keys of -NaN weigh nothing)
-        const int i = __ffsll(__ballot(enough)) - 1;  // the last lane is past hi
-        const u64 top_k = (u64)lo + (u64)step * (i + 1);
-        lo += step * i;
-        hi = top_k < hi ? (unsigned)top_k : hi;
-      }
-      if (hi > t_key) t_key = hi, ties = ~0ull;
-    }
-    // the cut's own bin, and the last index of the ties that stay
-    const int bin = t_key ? bin0 - bin_of(order_value(t_key), per_unit) : kLogitBins;
-    const bool in_lds = t_key &&  // the tokens around the cut are candidates (else the row itself is looked through)
-                         bin >= 0 && bin < kLogitBins && fetch(bin);
-    if (t_key) {
-      u64 n_ties = 0;
-      if (in_lds) {
-        for (int i = tid; i < sh.n; i += kRowThreads) n_ties += sh.key[i] == t_key;
-      } else {
-        for (int i = tid; i < V; i += kRowThreads) n_ties += usable(z[i]) && order_key(z[i]) == t_key;
-      }
-      n_ties = all_sum(n_ties);
-      if (ties < n_ties) {
-        u64 want = ties;
-        const unsigned top_index = (unsigned)(kMostVocab - 1);  // smaller indexes first: keys count downwards
-        const unsigned k = in_lds ? find_key(sh.n, 0, 20, [&](int i) { return top_index - sh.index[i]; },
-                                             [&](int i) { return sh.key[i] == t_key ? 1ull : 0ull; }, want, sh, tid, lane, wave)
-                                  : find_key(V, 0, 20, [&](int i) { return top_index - (unsigned)i; },
-                                             [&](int i) { return usable(z[i]) && order_key(z[i]) == t_key ? 1ull : 0ull; }, want, sh, tid, lane, wave);
-        last = top_index - k;
+        last = (unsigned)(kMostVocab - 1) - key;
       }
     }
     // kept weight of every stretch
     if (t_key) {
-      for (int i = tid; i < NS; i += kRowThreads) sh.inside[i] = 0;
       __syncthreads();
       if (in_lds) {
+        const int bin = held;
+        for (int i = tid; i < NS; i += kRowThreads) sh.inside[i] = 0;
+        __syncthreads();
         for (int i = tid; i < sh.n; i += kRowThreads)
-          if (sh.key[i] > t_key || (sh.key[i] == t_key && sh.index[i] <= last)) atomicAdd(&sh.inside[sh.index[i] / kStretch], row_weight(order_value(sh.key[i])));
+          if (sh.key[i] > t_key || (sh.key[i] == t_key && sh.index[i] <= last)) atomicAdd(&sh.inside[sh.index[i] / kStretch], row_weight(sh.key[i]));
         __syncthreads();
         for (int i = wave; i < NS; i += kRowWaves) {
           double m = 0;
@@ -536,54 +569,56 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
         for (int i = wave; i < NS; i += kRowWaves) {
           double m = 0;
           for (int x = i * kStretch + lane; x < min(V, (i + 1) * kStretch); x += 64) {
-            const float v = z[x];
-            if (!usable(v)) continue;
-            const unsigned k = order_key(v);
-            if (k > t_key || (k == t_key && (unsigned)x <= last)) m += (double)row_weight(v);
+            const unsigned k = usable(z[x]) ? order_key(z[x]) : 0;
+            if (k > t_key || (k == t_key && (unsigned)x <= last)) m += (double)row_weight(k);
           }
           m = wave_sum(m);
           if (lane == 0) sh.kept[i] = m;
         }
       }
-      __syncthreads();
     }
-  }
-  if (!t_key) {
-    if (tid < NS) sh.kept[tid] = whole_mine;
-    __syncthreads();
-  }
-
-  // ---- the draw ------------------------------------------------------------------------------------------------------------------
-  if (tid == 0) {  // (a sum in the order of the stretches)
-    double all = 0;
-    for (int i = 0; i < NS; ++i) all += sh.kept[i];
-    const float u = a.uniform[b];
-    const double target = u > 0.f ? (double)fminf(u, 1.f) * all : 0.0;
-    double before = 0, start = 0;
-    int pick = 0;
-    for (int i = 0; i < NS; ++i) {
-      if (sh.kept[i] > 0) {
-        pick = i, start = before;
-        if (before + sh.kept[i] > target) break;
-      }
-      before += sh.kept[i];
-    }
-    sh.n = pick;
-    sh.wave_d[0] = all;
-    sh.wave_d[1] = target - start;
   }
   __syncthreads();
-  const int pick = sh.n, first = pick * kStretch;
-  const double all = sh.wave_d[0], offset = sh.wave_d[1];
-  const float local = sh.top[pick];
-  u64 w[kStretch / kRowThreads], sum = 0;
-  float v[kStretch / kRowThreads];
+
+  // ---- the draw ------------------------------------------------------------------------------------------------------------------
+  // the stretch: four per lane, the same sums in every wave
+  constexpr int SPL = kMostStretches / 64;
+  double part[SPL], lane_sum = 0;
 #pragma unroll
-  for (int i = 0; i < kStretch / kRowThreads; ++i) {
-    const int x = first + tid * (kStretch / kRowThreads) + i;
-    v[i] = x < V ? z[x] : -INFINITY;
+  for (int i = 0; i < SPL; ++i) part[i] = lane * SPL + i < NS ? sh.kept[lane * SPL + i] : 0.0, lane_sum += part[i];
+  double upto = lane_sum;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double x = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += x;
+  }
+  const double all = __shfl(upto, 63, 64);
+  const float u = a.uniform[b];
+  const double wanted = u > 0.f ? (double)fminf(u, 1.f) * all : 0.0;
+  int pick = -1;       // of this lane: its first stretch that reaches past the number, else its last with any weight
+  double start = 0, run = upto - lane_sum;
+  bool reached = false;
+#pragma unroll
+  for (int i = 0; i < SPL; ++i) {
+    if (part[i] > 0 && !reached) pick = lane * SPL + i, start = run, reached = run + part[i] > wanted;
+    run += part[i];
+  }
+  const u64 past = __ballot(reached), some = __ballot(pick >= 0);
+  const int from = past ? __ffsll(past) - 1 : 63 - __clzll((long long)some);
+  pick = __shfl(pick, from, 64);
+  const double offset = wanted - __shfl(start, from, 64);
+  const int first = pick * kStretch;
+  // the token: some in a row per thread
+  constexpr int TPT = kStretch / kRowThreads;
+  const float local = sh.top[pick];
+  u64 w[TPT], sum = 0;
+  float v[TPT];
+#pragma unroll
+  for (int i = 0; i < TPT; ++i) v[i] = first + tid * TPT + i < V ? z[first + tid * TPT + i] : -INFINITY;
+#pragma unroll
+  for (int i = 0; i < TPT; ++i) {
     const unsigned k = usable(v[i]) ? order_key(v[i]) : 0;
-    w[i] = usable(v[i]) && (k > t_key || (k == t_key && (unsigned)x <= last)) ? fixed_of(weight_of(v[i], local, per_t)) : 0;
+    w[i] = k && (k > t_key || (k == t_key && (unsigned)(first + tid * TPT + i) <= last)) ? fixed_of(weight_of(v[i], local, per_t, powers)) : 0;
     sum += w[i];
   }
   u64 whole_stretch;
@@ -593,9 +628,9 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
   if (target >= whole_stretch) target = whole_stretch - 1;
   if (target < before || target >= before + sum) return;
 #pragma unroll
-  for (int i = 0; i < kStretch / kRowThreads; ++i) {
+  for (int i = 0; i < TPT; ++i) {
     if (target >= before && target < before + w[i])
-      answer(first + tid * (kStretch / kRowThreads) + i, (float)log(weight_of(v[i], top, per_t) * kOne / all));
+      answer(first + tid * TPT + i, (float)log(weight_of(v[i], top, per_t, powers) * kOne / all));
     before += w[i];
   }
 }
