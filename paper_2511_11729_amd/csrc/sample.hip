@@ -12,6 +12,7 @@
 // What bounds it: HBM for the logits in the first launch, with the exponential in 64 bits close behind it (20 instructions per token: 20 us for
 // 256 rows of 152064 against 26 us of reading); in the second the latency of its steps.
 #include <mutex>
+#include <type_traits>
 
 #include "ctx.h"
 #include "device_utils.h"
@@ -26,7 +27,7 @@ constexpr int kMostStretches = kMostVocab / kStretch;
 constexpr int kLogitBins = 256;     // of a stretch, downwards from its maximum
 constexpr int kCandidates = 8192;   // tokens of one bin that the second launch holds in LDS
 constexpr int kDigits = 2048;       // bins of a search: 11 bits
-constexpr int kRowThreads = 512, kRowWaves = kRowThreads / 64;
+constexpr int kRowThreads = 1024, kRowWaves = kRowThreads / 64;
 constexpr double kOne = (double)(1ull << 50);  // weight 1 in fixed point: 2^12 of them and more fit 64 bits
 
 // Order of the logits as unsigned integers; both zeros alike.
@@ -63,11 +64,12 @@ __device__ __forceinline__ double exp2_32nds(double t, const double* powers) {
   const double p = fma(fma(fma(fma(fma(c5, f, c4), f, c3), f, c2), f, c1), f, 1.0);
   return __builtin_amdgcn_ldexp(p * powers[i & 31], i >> 5);
 }
-// weight of a usable logit relative to `top`; per_t = 32 log2(e) / temperature
+// weight of a usable logit relative to `top`, which is not infinite; per_t = 32 log2(e) / temperature
 __device__ __forceinline__ double weight_of(float v, float top, double per_t, const double* powers) {
-  if (top == INFINITY) return v == top ? 1.0 : 0.0;
   return exp2_32nds(((double)v - (double)top) * per_t, powers);
 }
+// A row with logits of +inf is one of them alone, at zero.
+__device__ __forceinline__ float finite_row(float v) { return v == INFINITY ? 0.f : -INFINITY; }
 __device__ __forceinline__ u64 fixed_of(double w) {  // w <= 1: added to 2^52, its integer part stands in the low bits, rounded
   return (u64)__double_as_longlong(fma(w, kOne, (double)(1ull << 52))) & ((1ull << 52) - 1);
 }
@@ -104,16 +106,58 @@ __device__ __forceinline__ RowSettings settings_of(const harli_sample_batch& a, 
 struct SampleWs {
   float* top;        // largest logit
   unsigned* usable;  // tokens that can be drawn
-  u64* weight;       // sum of their weights
-  u64* bin_weight;   // [kLogitBins]
+  double* weight;      // sum of their weights, in fixed point relative to the largest
+  double* bin_weight;  // [kLogitBins]
   unsigned short* bin_count;
   int n;             // stretches per row
 };
 
-__device__ __forceinline__ u64 wave_sum64(u64 v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+// Lane moves of the vector ALU (not of LDS): a step of a scan adds what the lanes `CTRL` below hold; lanes without one add zero.
+template <int CTRL, int ROWS, typename T>
+__device__ __forceinline__ T lanes_below(T v) {
+  if constexpr (sizeof(T) == 8) {
+    const u64 u = __builtin_bit_cast(u64, v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)u, CTRL, ROWS, 0xf, false);
+    const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), CTRL, ROWS, 0xf, false);
+    return __builtin_bit_cast(T, (u64)hi << 32 | lo);
+  } else {
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+  }
+}
+template <typename T>
+__device__ __forceinline__ T row_scan(T v) {  // inclusive, inside rows of 16 lanes
+  v += lanes_below<0x111, 0xf>(v);
+  v += lanes_below<0x112, 0xf>(v);
+  v += lanes_below<0x114, 0xf>(v);
+  v += lanes_below<0x118, 0xf>(v);
   return v;
+}
+template <typename T>
+__device__ __forceinline__ T wave_scan(T v) {  // inclusive
+  v = row_scan(v);
+  v += lanes_below<0x142, 0xa>(v);  // the row before, to the second and fourth
+  v += lanes_below<0x143, 0xc>(v);  // the half before, to the third and fourth
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ T lane_value(T v, int lane) {  // lane: uniform
+  if constexpr (sizeof(T) == 8) {
+    const u64 u = __builtin_bit_cast(u64, v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)u, lane), hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(u >> 32), lane);
+    return __builtin_bit_cast(T, (u64)hi << 32 | lo);
+  } else {
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+  }
+}
+__device__ __forceinline__ float wave_top(float v) {  // of values that are not NaN
+  auto step = [&](auto ctrl) { v = fmaxf(v, __uint_as_float((unsigned)__builtin_amdgcn_update_dpp((int)0xff800000, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, false))); };
+  step(std::integral_constant<int, 0x111>{});
+  step(std::integral_constant<int, 0x112>{});
+  step(std::integral_constant<int, 0x114>{});
+  step(std::integral_constant<int, 0x118>{});
+  step(std::integral_constant<int, 0x142>{});
+  step(std::integral_constant<int, 0x143>{});
+  return lane_value(v, 63);
 }
 
 constexpr int kStretchThreads = 256, kPer = kStretch / kStretchThreads;
@@ -135,7 +179,9 @@ __global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) v[i] = i * kStretchThreads + tid < n ? z[i * kStretchThreads + tid] : -INFINITY;
+    for (int i = 0; i < kPer; ++i) v[i] = z[min(i * kStretchThreads + tid, n - 1)];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) v[i] = i * kStretchThreads + tid < n ? v[i] : -INFINITY;
   }
   const RowSettings s = settings_of(a, b);
   bin_weight[tid] = 0, bin_count[tid] = 0;
@@ -143,20 +189,24 @@ __global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample
   float top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) top = fmaxf(top, v[i]);  // (NaN is the other operand)
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  top = wave_top(top);
   if (lane == 0) s_top[wave] = top;
   __syncthreads();
   top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
   const size_t at = (size_t)b * ws.n + blockIdx.x;
   if (tid == 0) ws.top[at] = top;
   if (s.greedy) return;
+  if (top == INFINITY) {  // (the bins of such a row: its tokens of +inf in the first, like the row's)
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) v[i] = finite_row(v[i]);
+    top = 0.f;
+  }
   const double per_t = kPerT / (double)s.t;
   const float per_unit = bins_per_unit(s.t);
   const int bin0 = bin_of(top, per_unit);
   u64 sum = 0;
   unsigned count = 0;
-#pragma unroll 4
+#pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const bool in = usable(v[i]);
     const u64 w = in ? fixed_of(weight_of(v[i], top, per_t, powers)) : 0;
@@ -164,22 +214,20 @@ __global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample
     count += in;
     if (s.cut) {
       const int bin = bin0 - bin_of(v[i], per_unit);
-      if (in && bin < kLogitBins) {
-        if (w) atomicAdd(&bin_weight[bin], w);
-        if (s.k) atomicAdd(&bin_count[bin], 1u);
-      }
+      if (bin < kLogitBins && w) atomicAdd(&bin_weight[bin], w);
+      if (s.k && in && bin < kLogitBins) atomicAdd(&bin_count[bin], 1u);
     }
   }
-  sum = wave_sum64(sum);
-  count = wave_sum(count);
-  if (lane == 0) s_weight[wave] = sum, s_n[wave] = count;
+  sum = wave_scan(sum);
+  count = wave_scan(count);
+  if (lane == 63) s_weight[wave] = sum, s_n[wave] = count;
   __syncthreads();
   if (tid == 0) {
-    ws.weight[at] = s_weight[0] + s_weight[1] + s_weight[2] + s_weight[3];
+    ws.weight[at] = (double)(s_weight[0] + s_weight[1] + s_weight[2] + s_weight[3]);
     ws.usable[at] = s_n[0] + s_n[1] + s_n[2] + s_n[3];
   }
   if (s.cut) {
-    ws.bin_weight[at * kLogitBins + tid] = bin_weight[tid];
+    ws.bin_weight[at * kLogitBins + tid] = (double)bin_weight[tid];
     if (s.k) ws.bin_count[at * kLogitBins + tid] = (unsigned short)bin_count[tid];
   }
 }
@@ -187,6 +235,10 @@ __global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample
 // ---- the second launch -----------------------------------------------------------------------------------------------------------
 // Its steps are short and depend on one another, so what it costs is their latency, and its own code: a launch finds the instruction cache
 // cold.  The three searches (for top-k, for top-p, for the last of equal logits) are therefore one loop around one search.
+constexpr int kPart = 1024;                        // tokens that a wave looks through at a time for those of a bin
+constexpr int kListed = kCandidates / kRowWaves;   // tokens of the bin a wave can hold: every wave has a list of its own
+constexpr float kExactBins = (float)(1 << 22);     // bins up to here are told apart by comparing with their borders
+
 struct RowShared {
   u64 digit[kDigits];
   double powers[32];
@@ -200,95 +252,74 @@ struct RowShared {
   unsigned bin_count[kLogitBins];
   double part[kRowThreads / kLogitBins][kLogitBins];
   unsigned part_n[kRowThreads / kLogitBins][kLogitBins];
-  u64 wave64[kRowWaves];
-  double wave_d[kRowWaves];
+  u64 tmp[kRowWaves];
   float wave_f[kRowWaves];
   unsigned wave_u[2 * kRowWaves];
   u64 found_above;
   double found_above_d;
   unsigned found;
-  int n;                          // candidates
+  int least;
+  unsigned overflow;  // a wave's list did not hold its tokens
 };
 
-// Sum of v over the threads before this one and over all (whole workgroup).
-__device__ __forceinline__ u64 scan_before64(u64 v, RowShared& sh, int lane, int wave, u64& all) {
-  u64 s = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const u64 x = __shfl_up(s, o, 64);
-    if (lane >= o) s += x;
-  }
+// Sum of v up to and with this thread's, and over all (whole workgroup); the order of the additions is fixed.
+template <typename T>
+__device__ __forceinline__ T block_scan(T v, RowShared& sh, int lane, int wave, T& all) {
+  static_assert(kRowWaves <= 16, "the waves' sums in a row of lanes");
+  v = wave_scan(v);
   __syncthreads();
-  if (lane == 63) sh.wave64[wave] = s;
+  T* tmp = reinterpret_cast<T*>(sh.tmp);
+  if (lane == 63) tmp[wave] = v;
   __syncthreads();
-  u64 before = 0;
-  all = 0;
-#pragma unroll
-  for (int w = 0; w < kRowWaves; ++w) {
-    if (w < wave) before += sh.wave64[w];
-    all += sh.wave64[w];
-  }
-  return before + s - v;
+  const T t = row_scan(lane < kRowWaves ? tmp[lane] : T(0));
+  all = lane_value(t, kRowWaves - 1);
+  const T before = lane_value(t, wave ? wave - 1 : 0);
+  return wave ? before + v : v;
 }
-__device__ __forceinline__ u64 all_sum(u64 v, RowShared& sh, int lane, int wave) {
-  v = wave_sum64(v);
-  __syncthreads();
-  if (lane == 0) sh.wave64[wave] = v;
-  __syncthreads();
-  v = 0;
-#pragma unroll
-  for (int w = 0; w < kRowWaves; ++w) v += sh.wave64[w];
-  return v;
-}
-__device__ __forceinline__ double all_sum(double v, RowShared& sh, int lane, int wave) {  // in a fixed order
-  v = wave_sum(v);
-  __syncthreads();
-  if (lane == 0) sh.wave_d[wave] = v;
-  __syncthreads();
-  v = 0;
-#pragma unroll
-  for (int w = 0; w < kRowWaves; ++w) v += sh.wave_d[w];
-  return v;
+template <typename T>
+__device__ __forceinline__ T all_sum(T v, RowShared& sh, int lane, int wave) {
+  T all;
+  (void)block_scan(v, sh, lane, wave, all);
+  return all;
 }
 
-// The digit, from the highest, at which what the higher ones hold is less than `want` and with it not; sh.digit is filled in.
-// found_above: what the higher ones hold.  want is within the whole.
-__device__ __forceinline__ void find_digit(u64 want, RowShared& sh, int tid, int lane, int wave) {
-  constexpr int BPT = kDigits / kRowThreads;
-  u64 h[BPT], sum = 0, all;
-#pragma unroll
-  for (int i = 0; i < BPT; ++i) h[i] = sh.digit[kDigits - 1 - (tid * BPT + i)], sum += h[i];
-  u64 above = scan_before64(sum, sh, lane, wave, all);
-  if (above < want && above + sum >= want) {
-#pragma unroll
-    for (int i = 0; i < BPT; ++i) {
-      if (above < want && above + h[i] >= want) sh.found = kDigits - 1 - (tid * BPT + i), sh.found_above = above;
-      above += h[i];
-    }
-  }
-  __syncthreads();
-}
-
-// Among n items, key(i) and amount(i) (0: not looked at): the key at which the amounts of higher keys are less than `want` and with its
-// own not; `want` becomes what is missing above it.  Keys agree with `common` from bit `bits` on.
+// Among the items i = from, from + step, .. < end of every thread, key(i) and amount(i) (0: not looked at): the key at which the amounts of
+// higher keys are less than `want` and with its own not; `want` becomes what is missing above it (a want beyond the whole counts as the
+// whole).  Keys agree with `common` from bit `bits` on.
 template <typename Key, typename Amount>
-__device__ __forceinline__ unsigned find_key(int n, unsigned common, int bits, Key key, Amount amount, u64& want, RowShared& sh, int tid, int lane, int wave) {
+__device__ __forceinline__ unsigned find_key(int from, int end, int step, unsigned common, int bits, Key key, Amount amount, u64& want, RowShared& sh,
+                                             int tid, int lane, int wave) {
   unsigned prefix = bits < 32 ? common >> bits << bits : 0;
 #pragma unroll 1
   while (bits > 0) {
     const int width = min(bits, 11), shift = bits - width;
-    for (int i = tid; i < kDigits; i += kRowThreads) sh.digit[i] = 0;
+    constexpr int DPT = kDigits / kRowThreads;  // digits per thread
+#pragma unroll
+    for (int i = 0; i < DPT; ++i) sh.digit[tid * DPT + i] = 0;
     __syncthreads();
 #pragma unroll 1
-    for (int i = tid; i < n; i += kRowThreads) {
+    for (int i = from; i < end; i += step) {
       const unsigned k = key(i);
       if (bits == 32 || (k >> bits) == (prefix >> bits)) {
         const u64 w = amount(i);
-        if (w) atomicAdd(&sh.digit[(k >> shift) & ((1u << width) - 1)], w);
+        if (w) atomicAdd(&sh.digit[kDigits - 1 - ((k >> shift) & ((1u << width) - 1))], w);  // the highest first
       }
     }
     __syncthreads();
-    find_digit(want, sh, tid, lane, wave);
+    u64 h[DPT], sum = 0, all;
+#pragma unroll
+    for (int i = 0; i < DPT; ++i) h[i] = sh.digit[tid * DPT + i], sum += h[i];
+    u64 above = block_scan(sum, sh, lane, wave, all) - sum;
+    want = min(want, all);
+    if (above < want && above + sum >= want) {
+#pragma unroll
+      for (int i = 0; i < DPT; ++i) {
+        if (above < want && above + h[i] >= want) sh.found = kDigits - 1 - (tid * DPT + i), sh.found_above = above;
+        above += h[i];
+      }
+    }
+    if (tid == 0 && all == 0) sh.found = 0, sh.found_above = 0;
+    __syncthreads();
     want -= sh.found_above;
     prefix |= sh.found << shift;
     bits = shift;
@@ -305,44 +336,48 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
   const RowSettings s = settings_of(a, b);
 
   // ---- the stretches together ----------------------------------------------------------------------------------------------------
-  const float mine = tid < NS ? ws.top[at0 + tid] : -INFINITY;
-  float top = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  float mine = tid < NS ? ws.top[at0 + tid] : -INFINITY;
+  float top = wave_top(mine);
   if (lane == 0) sh.wave_f[wave] = top;
   if (tid < 32) sh.powers[tid] = kPowers.v[tid];
-  if (tid == 0) sh.found = 0xffffffffu, sh.n = NS;
+  if (tid == 0) sh.found = 0xffffffffu, sh.least = NS;
   __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kRowWaves; ++w) top = fmaxf(top, sh.wave_f[w]);
-  auto answer = [&](int token, float logprob) {
-    a.token[b] = token;
-    if (a.logprob) a.logprob[b] = logprob;
-  };
+  top = wave_top(lane < kRowWaves ? sh.wave_f[lane] : -INFINITY);
   if (top == -INFINITY) {
-    if (tid == 0) answer(-1, -INFINITY);
+    if (tid == 0) {
+      a.token[b] = -1;
+      if (a.logprob) a.logprob[b] = -INFINITY;
+    }
     return;
   }
   if (s.greedy) {
-    if (mine == top) atomicMin(&sh.n, tid);
+    if (mine == top) atomicMin(&sh.least, tid);
     __syncthreads();
-    const int first = sh.n * kStretch;
+    const int first = sh.least * kStretch;
     for (int i = first + tid; i < min(V, first + kStretch); i += kRowThreads)
       if (z[i] == top) atomicMin(&sh.found, (unsigned)i);
     __syncthreads();
-    if (tid == 0) answer((int)sh.found, 0.f);
+    if (tid == 0) {
+      a.token[b] = (int)sh.found;
+      if (a.logprob) a.logprob[b] = 0.f;
+    }
     return;
   }
+  const bool infinite = top == INFINITY;  // uniform
+  auto logit = [&](int i) { return infinite ? finite_row(z[i]) : z[i]; };
+  if (infinite) mine = finite_row(mine), top = 0.f;
   const double per_t = kPerT / (double)s.t;
   const double* powers = sh.powers;
   const float per_unit = bins_per_unit(s.t);
   const int bin0 = bin_of(top, per_unit);
   double whole_mine = 0;
   if (tid < NS) {
+    const bool some = usable(mine);
+    const double scale = some ? weight_of(mine, top, per_t, powers) : 0.0;
     sh.top[tid] = mine;
-    sh.below[tid] = usable(mine) ? bin0 - bin_of(mine, per_unit) : kLogitBins;
-    sh.scale[tid] = usable(mine) ? weight_of(mine, top, per_t, powers) : 0.0;
-    whole_mine = (double)ws.weight[at0 + tid] * sh.scale[tid];
+    sh.below[tid] = some ? bin0 - bin_of(mine, per_unit) : kLogitBins;
+    sh.scale[tid] = scale;
+    whole_mine = some ? ws.weight[at0 + tid] * scale : 0.0;
     sh.kept[tid] = whole_mine;
   }
   auto row_weight = [&](unsigned key) { return fixed_of(weight_of(order_value(key), top, per_t, powers)); };
@@ -352,28 +387,31 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
   if (s.cut) {
     double among = all_sum(whole_mine, sh, lane, wave);  // weight of the tokens that top-k leaves, in the row's fixed point
     {  // bins of the row
+      constexpr int NG = kRowThreads / kLogitBins;
       const int g = tid & (kLogitBins - 1), grp = tid / kLogitBins;
       double m = 0;
       unsigned c = 0;
 #pragma unroll 4
-      for (int i = grp; i < NS; i += kRowThreads / kLogitBins) {
+      for (int i = grp; i < NS; i += NG) {
         const int j = g - sh.below[i];
-        if (j >= 0) {
-          m += (double)ws.bin_weight[(at0 + i) * kLogitBins + j] * sh.scale[i];
-          if (s.k) c += ws.bin_count[(at0 + i) * kLogitBins + j];
-        }
+        const size_t e = (at0 + i) * kLogitBins + max(j, 0);
+        const double x = ws.bin_weight[e];
+        const unsigned n = s.k ? ws.bin_count[e] : 0;
+        m += j >= 0 ? x * sh.scale[i] : 0.0;
+        c += j >= 0 ? n : 0;
       }
       sh.part[grp][g] = m, sh.part_n[grp][g] = c;
       __syncthreads();
       if (tid < kLogitBins) {
         m = 0, c = 0;
 #pragma unroll
-        for (int x = 0; x < kRowThreads / kLogitBins; ++x) m += sh.part[x][tid], c += sh.part_n[x][tid];
+        for (int x = 0; x < NG; ++x) m += sh.part[x][tid], c += sh.part_n[x][tid];
         sh.bin_weight[tid] = m, sh.bin_count[tid] = c;
       }
     }
     u64 ties = ~0ull;  // how many of the tokens equal to t_key stay
-    int held = -1;     // the bin whose tokens are in LDS
+    int held = -1;     // the bin whose tokens are in LDS, and this wave's number of them
+    int listed = 0;
     bool in_lds = false;
 #pragma unroll 1
     for (int phase = 0; phase < 3; ++phase) {
@@ -385,25 +423,18 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
         if ((u64)s.k >= all_sum((u64)(tid < NS && usable(mine) ? ws.usable[at0 + tid] : 0), sh, lane, wave)) continue;  // (as many as there are)
         want = s.k;
         u64 all;
-        const u64 n = tid < kLogitBins ? sh.bin_count[tid] : 0, before = scan_before64(n, sh, lane, wave, all);
-        if (before < want && before + n >= want) sh.found = tid, sh.found_above = before;
+        const u64 n = tid < kLogitBins ? sh.bin_count[tid] : 0, upto = block_scan(n, sh, lane, wave, all);
+        if (upto - n < want && upto >= want) sh.found = tid, sh.found_above = upto - n;
         __syncthreads();
         if (want <= all) bin = sh.found;
       } else if (phase == 1) {  // top-p
         if (!(s.p < 1.f)) continue;
         want_d = fmax((double)s.p * among, 1.0);  // (the first token in any case)
+        double all;
         __syncthreads();
-        const double v = tid < kLogitBins ? sh.bin_weight[tid] : 0.0;
-        double upto = v;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-          const double x = __shfl_up(upto, o, 64);
-          if (lane >= o) upto += x;
-        }
-        if (lane == 63) sh.wave_d[wave] = upto;
+        const double v = tid < kLogitBins ? sh.bin_weight[tid] : 0.0, upto = block_scan(v, sh, lane, wave, all);
         if (tid == 0) sh.found = kLogitBins;
         __syncthreads();
-        for (int w = 0; w < wave; ++w) upto += sh.wave_d[w];
         if (v > 0 && upto >= want_d) atomicMin(&sh.found, (unsigned)tid);
         __syncthreads();
         bin = sh.found;
@@ -427,100 +458,80 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
         if (!t_key) break;
         bin = bin0 - bin_of(order_value(t_key), per_unit);
       }
+      const float border = (float)(bin0 - bin);
+      if (!(fabsf(border) < kExactBins)) bin = kLogitBins;
 
       // ---- the tokens of the bin, in LDS (their order there is of no account)
       if (bin < kLogitBins && bin != held) {
-        __syncthreads();
         held = bin;
-        if (tid == 0) sh.n = 0;
+        listed = 0;
+        __syncthreads();
+        if (tid == 0) sh.overflow = 0;
         __syncthreads();
 #pragma unroll 1
-        for (int i = wave; i < NS; i += kRowWaves) {  // a wave per stretch
-          const int j = bin - sh.below[i];
+        for (int lo = wave * kPart; lo < V; lo += kRowWaves * kPart) {
+          const int i = lo / kStretch, j = bin - sh.below[i];
           if (j < 0) continue;
           const size_t e = (at0 + i) * kLogitBins + j;
           if (s.k ? ws.bin_count[e] == 0 : ws.bin_weight[e] == 0) continue;
-          // all of the stretch in flight, then a bit per token, then their places with one addition to the common count
-          constexpr int R = kStretch / 64;
-          const int lo = i * kStretch, hi = min(V, lo + kStretch);
-          const bool wide = hi - lo == kStretch && (uintptr_t)(z + lo) % 16 == 0;
+          constexpr int R = kPart / 64;
           float v[R];
-          if (wide) {
 #pragma unroll
-            for (int r = 0; r < R / 4; ++r) {
-              const float4 x = reinterpret_cast<const float4*>(z + lo)[r * 64 + lane];
-              v[4 * r] = x.x, v[4 * r + 1] = x.y, v[4 * r + 2] = x.z, v[4 * r + 3] = x.w;
+          for (int r = 0; r < R; ++r) v[r] = z[min(lo + r * 64 + lane, V - 1)];
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const int x = lo + r * 64 + lane;
+            const float f = infinite ? finite_row(v[r]) : v[r], scaled = f * per_unit;
+            const bool in = scaled >= border && scaled < border + 1.f && x < V;
+            const u64 who = __ballot(in);
+            if (who) {
+              const int at = listed + (int)__popcll(who & ((1ull << lane) - 1));
+              if (in && at < kListed) sh.key[wave * kListed + at] = order_key(f), sh.index[wave * kListed + at] = (unsigned)x;
+              listed += __popcll(who);
             }
-          } else {
-#pragma unroll
-            for (int r = 0; r < R; ++r) v[r] = z[min(lo + r * 64 + lane, hi - 1)];
           }
-          const int target = bin0 - bin, first = wide ? lane * 4 : lane;
-          u64 in = 0;
-#pragma unroll
-          for (int r = 0; r < R; ++r) in |= (u64)(usable(v[r]) && bin_of(v[r], per_unit) == target) << r;
-          if (!wide) {  // what lies behind the row repeated its last token
-            const int n = lo + lane < hi ? (hi - lo - lane + 63) / 64 : 0;
-            if (n < 64) in &= (1ull << n) - 1;
-          }
-          const int mine_n = __popcll(in);
-          int at = mine_n;
-#pragma unroll
-          for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(at, o, 64);
-            if (lane >= o) at += x;
-          }
-          int base = 0;
-          if (lane == 63) base = atomicAdd(&sh.n, at);
-          at += __shfl(base, 63, 64) - mine_n;
-#pragma unroll
-          for (int r = 0; r < R; ++r)
-            if (in >> r & 1) {
-              if (at < kCandidates) sh.key[at] = order_key(v[r]), sh.index[at] = (unsigned)(lo + first + (wide ? (r >> 2) * 256 + (r & 3) : r * 64));
-              ++at;
-            }
         }
+        if (listed > kListed && lane == 0) sh.overflow = 1;
         __syncthreads();
       }
-      in_lds = bin < kLogitBins && sh.n <= kCandidates;
-      const int n = in_lds ? sh.n : V;
-      // what the search looks at: the candidates, or all of the row
-      auto key_at = [&](int i) { return in_lds ? sh.key[i] : usable(z[i]) ? order_key(z[i]) : 0u; };
+      in_lds = bin < kLogitBins && sh.overflow == 0;
+      // what the search looks at: the listed tokens, every wave its own, or all of the row
+      const int from = in_lds ? wave * kListed + lane : tid, end = in_lds ? wave * kListed + listed : V, step = in_lds ? 64 : kRowThreads;
+      auto key_at = [&](int i) {
+        if (in_lds) return sh.key[i];
+        const float v = logit(i);
+        return usable(v) ? order_key(v) : 0u;
+      };
       const int wide_sum = in_lds ? 0 : 8;  // sums over a whole row: 2^20 weights fit 62 bits
       unsigned common = 0;
       int bits = 32;
       if (phase == 2) {
         u64 equal = 0;
-        for (int i = tid; i < n; i += kRowThreads) equal += key_at(i) == t_key;
+        for (int i = from; i < end; i += step) equal += key_at(i) == t_key;
         if (ties >= all_sum(equal, sh, lane, wave)) break;  // all of them
         want = ties;
         bits = 20;
-      } else if (in_lds) {  // the highest bit in which the candidates differ
-        unsigned lo = 0xffffffffu, hi = 0;
-        for (int i = tid; i < n; i += kRowThreads) lo = min(lo, sh.key[i]), hi = max(hi, sh.key[i]);
+      } else if (in_lds) {  // the highest bit in which the listed tokens differ
+        unsigned ones = 0, zeros = 0;
+        for (int i = from; i < end; i += step) ones |= sh.key[i], zeros |= ~sh.key[i];
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) lo = min(lo, (unsigned)__shfl_xor((int)lo, o, 64)), hi = max(hi, (unsigned)__shfl_xor((int)hi, o, 64));
-        if (lane == 0) sh.wave_u[wave] = lo, sh.wave_u[kRowWaves + wave] = hi;
+        for (int o = 1; o < 64; o <<= 1) ones |= (unsigned)__shfl_xor((int)ones, o, 64), zeros |= (unsigned)__shfl_xor((int)zeros, o, 64);
+        if (lane == 0) sh.wave_u[wave] = ones, sh.wave_u[kRowWaves + wave] = zeros;
         __syncthreads();
+        ones = zeros = 0;
 #pragma unroll
-        for (int w = 0; w < kRowWaves; ++w) lo = min(lo, sh.wave_u[w]), hi = max(hi, sh.wave_u[kRowWaves + w]);
-        common = hi;
-        bits = lo == hi ? 0 : 32 - __clz((int)(lo ^ hi));
+        for (int w = 0; w < kRowWaves; ++w) ones |= sh.wave_u[w], zeros |= sh.wave_u[kRowWaves + w];
+        common = ones;
+        bits = (ones & zeros) == 0 ? 0 : 32 - __clz((int)(ones & zeros));
       }
       if (phase == 0 && in_lds) want -= sh.found_above;
       if (phase == 1) {
-        u64 have = 0;
-        for (int i = tid; i < n; i += kRowThreads) {
-          const unsigned k = key_at(i);
-          if (k) have += row_weight(k) >> wide_sum;
-        }
-        have = all_sum(have, sh, lane, wave);
         const double x = in_lds ? ceil(want_d - sh.found_above_d) : ceil(want_d / 256);
-        want = x < 1.0 ? 1 : x >= (double)have ? have : (u64)x;
-        if (have == 0) continue;  // (weights that round to nothing: they are not drawn anyway)
+        want = x < 1.0 ? 1 : (u64)x;
       }
       const unsigned key = find_key(
-          n, common, bits, [&](int i) { return phase == 2 ? (unsigned)(kMostVocab - 1) - (in_lds ? sh.index[i] : (unsigned)i) : key_at(i); },
+          from, end, step, common, bits,
+          [&](int i) { return phase == 2 ? (unsigned)(kMostVocab - 1) - (in_lds ? sh.index[i] : (unsigned)i) : key_at(i); },
           [&](int i) -> u64 {
             const unsigned k = key_at(i);
             return phase == 2 ? k == t_key : k == 0 ? 0 : phase == 0 ? 1 : row_weight(k) >> wide_sum;
@@ -528,16 +539,12 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
           want, sh, tid, lane, wave);
       if (phase == 0) {
         t_key = key, ties = want;
-        double w = 0;  // what the first k weigh: above the bin, and the candidates above the cut (or the row's tokens above it)
-        u64 w64 = 0;
-        for (int i = tid; i < n; i += kRowThreads) {
+        // what the first k weigh: above the bin, and the listed tokens above the cut (or the row's tokens above it)
+        double w = in_lds && tid < bin ? sh.bin_weight[tid] : 0.0;
+        for (int i = from; i < end; i += step) {
           const unsigned k = key_at(i);
-          if (k > key) {
-            if (in_lds) w64 += row_weight(k);
-            else w += (double)row_weight(k);
-          }
+          if (k > key) w += (double)row_weight(k);
         }
-        if (in_lds) w = (double)w64 + (tid < bin ? sh.bin_weight[tid] : 0.0);
         among = all_sum(w, sh, lane, wave) + (double)ties * (double)row_weight(key);
       } else if (phase == 1) {
         const u64 w = row_weight(key) >> wide_sum, of_key = w ? (want + w - 1) / w : ~0ull;
@@ -554,26 +561,33 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
         const int bin = held;
         for (int i = tid; i < NS; i += kRowThreads) sh.inside[i] = 0;
         __syncthreads();
-        for (int i = tid; i < sh.n; i += kRowThreads)
-          if (sh.key[i] > t_key || (sh.key[i] == t_key && sh.index[i] <= last)) atomicAdd(&sh.inside[sh.index[i] / kStretch], row_weight(sh.key[i]));
+        for (int i = wave * kListed + lane; i < wave * kListed + listed; i += 64) {
+          const unsigned k = sh.key[i], x = sh.index[i];
+          if (k > t_key || (k == t_key && x <= last)) atomicAdd(&sh.inside[x / kStretch], row_weight(k));
+        }
         __syncthreads();
+#pragma unroll 1
         for (int i = wave; i < NS; i += kRowWaves) {
           double m = 0;
 #pragma unroll
-          for (int j = 0; j < kLogitBins; j += 64)
-            if (j + lane < bin - sh.below[i]) m += (double)ws.bin_weight[(at0 + i) * kLogitBins + j + lane];
-          m = wave_sum(m);
-          if (lane == 0) sh.kept[i] = m * sh.scale[i] + (double)sh.inside[i];
+          for (int j = 0; j < kLogitBins; j += 64) {
+            const double x = ws.bin_weight[(at0 + i) * kLogitBins + j + lane];
+            m += j + lane < bin - sh.below[i] ? x : 0.0;
+          }
+          m = wave_scan(m);
+          if (lane == 63) sh.kept[i] = m * sh.scale[i] + (double)sh.inside[i];
         }
       } else {
+#pragma unroll 1
         for (int i = wave; i < NS; i += kRowWaves) {
           double m = 0;
           for (int x = i * kStretch + lane; x < min(V, (i + 1) * kStretch); x += 64) {
-            const unsigned k = usable(z[x]) ? order_key(z[x]) : 0;
+            const float v = logit(x);
+            const unsigned k = usable(v) ? order_key(v) : 0;
             if (k > t_key || (k == t_key && (unsigned)x <= last)) m += (double)row_weight(k);
           }
-          m = wave_sum(m);
-          if (lane == 0) sh.kept[i] = m;
+          m = wave_scan(m);
+          if (lane == 63) sh.kept[i] = m;
         }
       }
     }
@@ -586,13 +600,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
   double part[SPL], lane_sum = 0;
 #pragma unroll
   for (int i = 0; i < SPL; ++i) part[i] = lane * SPL + i < NS ? sh.kept[lane * SPL + i] : 0.0, lane_sum += part[i];
-  double upto = lane_sum;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double x = __shfl_up(upto, o, 64);
-    if (lane >= o) upto += x;
-  }
-  const double all = __shfl(upto, 63, 64);
+  const double upto = wave_scan(lane_sum), all = lane_value(upto, 63);
   const float u = a.uniform[b];
   const double wanted = u > 0.f ? (double)fminf(u, 1.f) * all : 0.0;
   int pick = -1;       // of this lane: its first stretch that reaches past the number, else its last with any weight
@@ -605,8 +613,8 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
   }
   const u64 past = __ballot(reached), some = __ballot(pick >= 0);
   const int from = past ? __ffsll(past) - 1 : 63 - __clzll((long long)some);
-  pick = __shfl(pick, from, 64);
-  const double offset = wanted - __shfl(start, from, 64);
+  pick = lane_value(pick, from);
+  const double offset = wanted - lane_value(start, from);
   const int first = pick * kStretch;
   // the token: some in a row per thread
   constexpr int TPT = kStretch / kRowThreads;
@@ -614,23 +622,28 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
   u64 w[TPT], sum = 0;
   float v[TPT];
 #pragma unroll
-  for (int i = 0; i < TPT; ++i) v[i] = first + tid * TPT + i < V ? z[first + tid * TPT + i] : -INFINITY;
+  for (int i = 0; i < TPT; ++i) v[i] = first + tid * TPT + i < V ? logit(first + tid * TPT + i) : -INFINITY;
 #pragma unroll
   for (int i = 0; i < TPT; ++i) {
     const unsigned k = usable(v[i]) ? order_key(v[i]) : 0;
     w[i] = k && (k > t_key || (k == t_key && (unsigned)(first + tid * TPT + i) <= last)) ? fixed_of(weight_of(v[i], local, per_t, powers)) : 0;
     sum += w[i];
   }
-  u64 whole_stretch;
-  u64 before = scan_before64(sum, sh, lane, wave, whole_stretch);
+  u64 whole_stretch, before = block_scan(sum, sh, lane, wave, whole_stretch) - sum;
   const double x = offset / sh.scale[pick];
   u64 target = x >= (double)whole_stretch ? whole_stretch - 1 : x > 0 ? (u64)x : 0;
   if (target >= whole_stretch) target = whole_stretch - 1;
   if (target < before || target >= before + sum) return;
 #pragma unroll
   for (int i = 0; i < TPT; ++i) {
-    if (target >= before && target < before + w[i])
-      answer(first + tid * TPT + i, (float)log(weight_of(v[i], top, per_t, powers) * kOne / all));
+    if (target >= before && target < before + w[i]) {
+      a.token[b] = first + tid * TPT + i;
+      if (a.logprob) {
+        // log of the sum: a logarithm in 32 bits and what the exponential in 64 leaves of it
+        const double sum1 = all / kOne, y = (double)logf((float)sum1), r = sum1 * exp2_32nds(-y * kPerT, powers) - 1.0;
+        a.logprob[b] = (float)(((double)v[i] - (double)top) * per_t / kPerT - y - (r - 0.5 * r * r));
+      }
+    }
     before += w[i];
   }
 }
@@ -650,8 +663,8 @@ SampleLayout sample_layout(int batch, int vocab, void* base) {
     l.bytes += al(bytes);
     return q;
   };
-  l.ws.bin_weight = reinterpret_cast<u64*>(take(n * kLogitBins * 8));
-  l.ws.weight = reinterpret_cast<u64*>(take(n * 8));
+  l.ws.bin_weight = reinterpret_cast<double*>(take(n * kLogitBins * 8));
+  l.ws.weight = reinterpret_cast<double*>(take(n * 8));
   l.ws.top = reinterpret_cast<float*>(take(n * 4));
   l.ws.usable = reinterpret_cast<unsigned*>(take(n * 4));
   l.ws.bin_count = reinterpret_cast<unsigned short*>(take(n * kLogitBins * 2));
