@@ -38,50 +38,58 @@ __device__ __forceinline__ unsigned order_key(float v) {
 __device__ __forceinline__ float order_value(unsigned k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 __device__ __forceinline__ bool usable(float v) { return v > -INFINITY; }  // (not NaN either)
 
-// 2^(j / 32), by the series of exp (constant expressions: the compiler's own doubles)
+// 2^(j / 64), by the series of exp (constant expressions: the compiler's own doubles)
+constexpr int kPowersN = 64;
+constexpr double kLn2 = 0.693147180559945309417;
 constexpr double exp_series(double x) {
   double sum = 1, term = 1;
   for (int i = 1; i < 24; ++i) term = term * x / i, sum += term;
   return sum;
 }
-constexpr double kLn2 = 0.693147180559945309417;
-struct PowerTable {
-  double v[32];
+struct Powers {
+  double v[kPowersN];
 };
-constexpr PowerTable make_powers() {
-  PowerTable t{};
-  for (int j = 0; j < 32; ++j) t.v[j] = exp_series(kLn2 * j / 32);
+constexpr Powers make_powers() {
+  Powers t{};
+  for (int j = 0; j < kPowersN; ++j) t.v[j] = exp_series(kLn2 * j / kPowersN);
   return t;
 }
-__constant__ PowerTable kPowers = make_powers();
+__constant__ Powers kPowers = make_powers();
 
-// 2^(t / 32): t = 32 e + j + f; the table's 2^(j / 32) times the series of exp(f ln 2 / 32) over |f| <= 1/2 to the fifth power (what
-// follows is below 3e-15).  `powers`: the table in LDS, where its 32 entries lie in banks of their own.
-__device__ __forceinline__ double exp2_32nds(double t, const double* powers) {
-  constexpr double l = kLn2 / 32, c1 = l, c2 = c1 * l / 2, c3 = c2 * l / 3, c4 = c3 * l / 4, c5 = c4 * l / 5;
-  const double n = rint(t), f = t - n;
-  const int i = (int)n;  // (far below the range it saturates: zero)
-  const double p = fma(fma(fma(fma(fma(c5, f, c4), f, c3), f, c2), f, c1), f, 1.0);
-  return __builtin_amdgcn_ldexp(p * powers[i & 31], i >> 5);
-}
-// weight of a usable logit relative to `top`, which is not infinite; per_t = 32 log2(e) / temperature
-__device__ __forceinline__ double weight_of(float v, float top, double per_t, const double* powers) {
-  return exp2_32nds(((double)v - (double)top) * per_t, powers);
-}
+// 2^(t / 64): t = 64 e + j + f; the table's 2^(j / 64) times the series of exp(f ln 2 / 64) over |f| <= 1/2 to the fourth power (what
+// follows is below 2^-44).  The coefficients come as kernel arguments, that is as scalar operands: as immediates every one of them
+// is moved into registers for every token.
+struct Series {
+  double c1, c2, c3, c4, two52;
+};
+constexpr Series kSeries = {kLn2 / 64, kLn2 / 64 * (kLn2 / 64) / 2, kLn2 / 64 * (kLn2 / 64) * (kLn2 / 64) / 6,
+                            kLn2 / 64 * (kLn2 / 64) * (kLn2 / 64) * (kLn2 / 64) / 24, (double)(1ull << 52)};
+struct Exp {
+  Series s;
+  const double* powers;  // the table in LDS
+  __device__ __forceinline__ double at(double t) const {
+    const double n = rint(t), f = t - n;
+    const int i = (int)n;  // (far below the range it saturates: zero)
+    const double p = fma(fma(fma(fma(s.c4, f, s.c3), f, s.c2), f, s.c1), f, 1.0);
+    return __builtin_amdgcn_ldexp(p * powers[i & (kPowersN - 1)], i >> 6);
+  }
+  // weight of a usable logit relative to `top`, which is not infinite; per_t = 64 log2(e) / temperature
+  __device__ __forceinline__ double weight(float v, float top, double per_t) const { return at(((double)v - (double)top) * per_t); }
+  // ... in fixed point: added to 2^52, the integer part of w * kOne stands in the low bits, rounded (w <= 1)
+  __device__ __forceinline__ u64 fixed(float v, float top, double per_t) const {
+    return (u64)__double_as_longlong(fma(weight(v, top, per_t), kOne, s.two52)) & ((1ull << 52) - 1);
+  }
+};
 // A row with logits of +inf is one of them alone, at zero.
 __device__ __forceinline__ float finite_row(float v) { return v == INFINITY ? 0.f : -INFINITY; }
-__device__ __forceinline__ u64 fixed_of(double w) {  // w <= 1: added to 2^52, its integer part stands in the low bits, rounded
-  return (u64)__double_as_longlong(fma(w, kOne, (double)(1ull << 52))) & ((1ull << 52) - 1);
-}
-
 // Bins of the logit for a row: their width is an eighth of the temperature, within 1/16 and 1/8 of the logit's unit, so that 256 of them span 16
 // units at least and one holds a few per cent of a vocabulary at most.  They lie on a grid common to all stretches.
 __device__ __forceinline__ float bins_per_unit(float t) { return fminf(fmaxf(8.f / t, 8.f), 16.f); }
 __device__ __forceinline__ int bin_of(float v, float per_unit) {  // monotone; kept inside the integers
-  return (int)floorf(fminf(fmaxf(v * per_unit, -5e8f), 5e8f));
+  return (int)floorf(__builtin_amdgcn_fmed3f(v * per_unit, -5e8f, 5e8f));
 }
 
-constexpr double kPerT = 32 * 1.4426950408889634074;
+constexpr double kPerT = 64 * 1.4426950408889634074;
 struct RowSettings {
   float t, p;
   double min_p;
@@ -107,8 +115,8 @@ struct SampleWs {
   float* top;        // largest logit
   unsigned* usable;  // tokens that can be drawn
   double* weight;      // sum of their weights, in fixed point relative to the largest
-  double* bin_weight;  // [kLogitBins]
-  unsigned short* bin_count;
+  double* upto_weight;         // [kLogitBins] weights of the bins up to each one
+  unsigned short* upto_count;  // [kLogitBins] tokens of them
   int n;             // stretches per row
 };
 
@@ -162,10 +170,10 @@ __device__ __forceinline__ float wave_top(float v) {  // of values that are not 
 
 constexpr int kStretchThreads = 256, kPer = kStretch / kStretchThreads;
 
-__global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample_batch a, SampleWs ws) {
+__global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample_batch a, SampleWs ws, Series series) {
   __shared__ float s_top[4];
   __shared__ u64 s_weight[4], bin_weight[kLogitBins];
-  __shared__ double powers[32];
+  __shared__ double powers[kPowersN];
   __shared__ unsigned s_n[4], bin_count[kLogitBins];
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, first = blockIdx.x * kStretch;
   const float* z = a.logits + (size_t)b * a.ld + first;
@@ -185,7 +193,7 @@ __global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample
   }
   const RowSettings s = settings_of(a, b);
   bin_weight[tid] = 0, bin_count[tid] = 0;
-  if (tid < 32) powers[tid] = kPowers.v[tid];
+  if (tid < kPowersN) powers[tid] = kPowers.v[tid];
   float top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) top = fmaxf(top, v[i]);  // (NaN is the other operand)
@@ -202,6 +210,7 @@ __global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample
     top = 0.f;
   }
   const double per_t = kPerT / (double)s.t;
+  const Exp ex{series, powers};
   const float per_unit = bins_per_unit(s.t);
   const int bin0 = bin_of(top, per_unit);
   u64 sum = 0;
@@ -209,12 +218,12 @@ __global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const bool in = usable(v[i]);
-    const u64 w = in ? fixed_of(weight_of(v[i], top, per_t, powers)) : 0;
+    const u64 w = in ? ex.fixed(v[i], top, per_t) : 0;
     sum += w;
     count += in;
     if (s.cut) {
       const int bin = bin0 - bin_of(v[i], per_unit);
-      if (bin < kLogitBins && w) atomicAdd(&bin_weight[bin], w);
+      if (in && bin < kLogitBins) atomicAdd(&bin_weight[bin], w);
       if (s.k && in && bin < kLogitBins) atomicAdd(&bin_count[bin], 1u);
     }
   }
@@ -227,8 +236,15 @@ __global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample
     ws.usable[at] = s_n[0] + s_n[1] + s_n[2] + s_n[3];
   }
   if (s.cut) {
-    ws.bin_weight[at * kLogitBins + tid] = (double)bin_weight[tid];
-    if (s.k) ws.bin_count[at * kLogitBins + tid] = (unsigned short)bin_count[tid];
+    static_assert(kLogitBins == kStretchThreads, "a bin per thread");
+    u64 w = wave_scan(bin_weight[tid]);
+    unsigned c = wave_scan(bin_count[tid]);
+    __syncthreads();
+    if (lane == 63) s_weight[wave] = w, s_n[wave] = c;
+    __syncthreads();
+    for (int x = 0; x < wave; ++x) w += s_weight[x], c += s_n[x];
+    ws.upto_weight[at * kLogitBins + tid] = (double)w;
+    if (s.k) ws.upto_count[at * kLogitBins + tid] = (unsigned short)c;
   }
 }
 
@@ -241,22 +257,22 @@ constexpr float kExactBins = (float)(1 << 22);     // bins up to here are told a
 
 struct RowShared {
   u64 digit[kDigits];
-  double powers[32];
+  double powers[kPowersN];
   unsigned key[kCandidates], index[kCandidates];
   float top[kMostStretches];
   int below[kMostStretches];      // bins from the row's first to the stretch's
   double scale[kMostStretches];   // weight of the stretch's largest logit in the row
   double kept[kMostStretches];
   u64 inside[kMostStretches];     // kept weight of the cut's own bin, in the row's fixed point
-  double bin_weight[kLogitBins];
-  unsigned bin_count[kLogitBins];
+  double upto_weight[kLogitBins];  // of the row's bins up to each one
+  unsigned upto_count[kLogitBins];
+  unsigned char some[kMostStretches];  // whether the stretch has tokens of the bin
   double part[kRowThreads / kLogitBins][kLogitBins];
   unsigned part_n[kRowThreads / kLogitBins][kLogitBins];
   u64 tmp[kRowWaves];
   float wave_f[kRowWaves];
   unsigned wave_u[2 * kRowWaves];
   u64 found_above;
-  double found_above_d;
   unsigned found;
   int least;
   unsigned overflow;  // a wave's list did not hold its tokens
@@ -327,7 +343,7 @@ __device__ __forceinline__ unsigned find_key(int from, int end, int step, unsign
   return prefix;
 }
 
-__global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a, SampleWs ws) {
+__global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a, SampleWs ws, Series series) {
   extern __shared__ __align__(16) char row_lds[];
   RowShared& sh = *reinterpret_cast<RowShared*>(row_lds);
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = a.vocab, NS = ws.n;
@@ -339,7 +355,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
   float mine = tid < NS ? ws.top[at0 + tid] : -INFINITY;
   float top = wave_top(mine);
   if (lane == 0) sh.wave_f[wave] = top;
-  if (tid < 32) sh.powers[tid] = kPowers.v[tid];
+  if (tid < kPowersN) sh.powers[tid] = kPowers.v[tid];
   if (tid == 0) sh.found = 0xffffffffu, sh.least = NS;
   __syncthreads();
   top = wave_top(lane < kRowWaves ? sh.wave_f[lane] : -INFINITY);
@@ -367,20 +383,20 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
   auto logit = [&](int i) { return infinite ? finite_row(z[i]) : z[i]; };
   if (infinite) mine = finite_row(mine), top = 0.f;
   const double per_t = kPerT / (double)s.t;
-  const double* powers = sh.powers;
+  const Exp ex{series, sh.powers};
   const float per_unit = bins_per_unit(s.t);
   const int bin0 = bin_of(top, per_unit);
   double whole_mine = 0;
   if (tid < NS) {
     const bool some = usable(mine);
-    const double scale = some ? weight_of(mine, top, per_t, powers) : 0.0;
+    const double scale = some ? ex.weight(mine, top, per_t) : 0.0;
     sh.top[tid] = mine;
     sh.below[tid] = some ? bin0 - bin_of(mine, per_unit) : kLogitBins;
     sh.scale[tid] = scale;
     whole_mine = some ? ws.weight[at0 + tid] * scale : 0.0;
     sh.kept[tid] = whole_mine;
   }
-  auto row_weight = [&](unsigned key) { return fixed_of(weight_of(order_value(key), top, per_t, powers)); };
+  auto row_weight = [&](unsigned key) { return ex.fixed(order_value(key), top, per_t); };
 
   // ---- the cut: logits with keys above t_key stay, and of those equal to it the ones up to index last ----------------------------
   unsigned t_key = 0, last = 0xffffffffu;
@@ -391,12 +407,12 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
       const int g = tid & (kLogitBins - 1), grp = tid / kLogitBins;
       double m = 0;
       unsigned c = 0;
-#pragma unroll 4
+#pragma unroll 5
       for (int i = grp; i < NS; i += NG) {
         const int j = g - sh.below[i];
         const size_t e = (at0 + i) * kLogitBins + max(j, 0);
-        const double x = ws.bin_weight[e];
-        const unsigned n = s.k ? ws.bin_count[e] : 0;
+        const double x = ws.upto_weight[e];
+        const unsigned n = s.k ? ws.upto_count[e] : 0;
         m += j >= 0 ? x * sh.scale[i] : 0.0;
         c += j >= 0 ? n : 0;
       }
@@ -406,8 +422,9 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
         m = 0, c = 0;
 #pragma unroll
         for (int x = 0; x < NG; ++x) m += sh.part[x][tid], c += sh.part_n[x][tid];
-        sh.bin_weight[tid] = m, sh.bin_count[tid] = c;
+        sh.upto_weight[tid] = m, sh.upto_count[tid] = c;
       }
+      __syncthreads();
     }
     u64 ties = ~0ull;  // how many of the tokens equal to t_key stay
     int held = -1;     // the bin whose tokens are in LDS, and this wave's number of them
@@ -422,24 +439,22 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
         if (!s.k) continue;
         if ((u64)s.k >= all_sum((u64)(tid < NS && usable(mine) ? ws.usable[at0 + tid] : 0), sh, lane, wave)) continue;  // (as many as there are)
         want = s.k;
-        u64 all;
-        const u64 n = tid < kLogitBins ? sh.bin_count[tid] : 0, upto = block_scan(n, sh, lane, wave, all);
-        if (upto - n < want && upto >= want) sh.found = tid, sh.found_above = upto - n;
+        if (tid < kLogitBins) {
+          const unsigned upto = sh.upto_count[tid], before = tid ? sh.upto_count[tid - 1] : 0;
+          if (before < want && upto >= want) sh.found = tid, sh.found_above = before;
+        }
         __syncthreads();
-        if (want <= all) bin = sh.found;
+        if (want <= sh.upto_count[kLogitBins - 1]) bin = sh.found;
       } else if (phase == 1) {  // top-p
         if (!(s.p < 1.f)) continue;
         want_d = fmax((double)s.p * among, 1.0);  // (the first token in any case)
-        double all;
         __syncthreads();
-        const double v = tid < kLogitBins ? sh.bin_weight[tid] : 0.0, upto = block_scan(v, sh, lane, wave, all);
         if (tid == 0) sh.found = kLogitBins;
         __syncthreads();
-        if (v > 0 && upto >= want_d) atomicMin(&sh.found, (unsigned)tid);
+        if (tid < kLogitBins && sh.upto_weight[tid] >= want_d) atomicMin(&sh.found, (unsigned)tid);
         __syncthreads();
         bin = sh.found;
-        if (tid == bin) sh.found_above_d = upto - v;
-      } else {  // the cut's own bin, for the last of equal logits and for the weights
+            } else {  // the cut's own bin, for the last of equal logits and for the weights
         if (s.min_p > 0.0) {
           // the smallest key whose weight is min_p or more: 64 keys at a time, the same search in every wave
           unsigned lo = 0, hi = order_key(top);  // lo: too small, hi: large enough
@@ -447,7 +462,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
           while (hi - lo > 1) {
             const unsigned step = (hi - lo + 63) / 64;
             const u64 k = (u64)lo + (u64)step * (lane + 1);
-            const bool enough = k >= hi || weight_of(order_value((unsigned)k), top, per_t, powers) >= s.min_p;  // (keys of NaN weigh nothing)
+            const bool enough = k >= hi || ex.weight(order_value((unsigned)k), top, per_t) >= s.min_p;  // (keys of NaN weigh nothing)
             const int i = __ffsll(__ballot(enough)) - 1;  // the last lane is past hi
             const u64 next = (u64)lo + (u64)step * (i + 1);
             lo += step * i;
@@ -467,20 +482,37 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
         listed = 0;
         __syncthreads();
         if (tid == 0) sh.overflow = 0;
+        if (tid < NS) {
+          const int j = bin - sh.below[tid];
+          const size_t e = (at0 + tid) * kLogitBins + max(j, 0);
+          bool some = j >= 0;
+          if (j > 0) some = s.k ? ws.upto_count[e] != ws.upto_count[e - 1] : ws.upto_weight[e] != ws.upto_weight[e - 1];
+          sh.some[tid] = some;
+        }
         __syncthreads();
-#pragma unroll 1
-        for (int lo = wave * kPart; lo < V; lo += kRowWaves * kPart) {
-          const int i = lo / kStretch, j = bin - sh.below[i];
-          if (j < 0) continue;
-          const size_t e = (at0 + i) * kLogitBins + j;
-          if (s.k ? ws.bin_count[e] == 0 : ws.bin_weight[e] == 0) continue;
-          constexpr int R = kPart / 64;
-          float v[R];
+        // the next part's tokens are in flight while this part's are looked at
+        constexpr int R = kPart / 64;
+        auto needed = [&](int lo) {
+          while (lo < V && !__builtin_amdgcn_readfirstlane(sh.some[lo / kStretch])) lo += kRowWaves * kPart;
+          return lo;
+        };
+        float v[R], ahead[R];
+        int lo = needed(wave * kPart);
 #pragma unroll
-          for (int r = 0; r < R; ++r) v[r] = z[min(lo + r * 64 + lane, V - 1)];
+        for (int r = 0; r < R; ++r) ahead[r] = z[min(lo + r * 64 + lane, V - 1)];
+#pragma unroll 1
+        while (lo < V) {
+          const int now = lo;
+          lo = needed(now + kRowWaves * kPart);
+#pragma unroll
+          for (int r = 0; r < R; ++r) v[r] = ahead[r];
+          if (lo < V) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) ahead[r] = z[min(lo + r * 64 + lane, V - 1)];
+          }
 #pragma unroll
           for (int r = 0; r < R; ++r) {
-            const int x = lo + r * 64 + lane;
+            const int x = now + r * 64 + lane;
             const float f = infinite ? finite_row(v[r]) : v[r], scaled = f * per_unit;
             const bool in = scaled >= border && scaled < border + 1.f && x < V;
             const u64 who = __ballot(in);
@@ -526,7 +558,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
       }
       if (phase == 0 && in_lds) want -= sh.found_above;
       if (phase == 1) {
-        const double x = in_lds ? ceil(want_d - sh.found_above_d) : ceil(want_d / 256);
+        const double x = in_lds ? ceil(want_d - (bin ? sh.upto_weight[bin - 1] : 0.0)) : ceil(want_d / 256);
         want = x < 1.0 ? 1 : (u64)x;
       }
       const unsigned key = find_key(
@@ -540,7 +572,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
       if (phase == 0) {
         t_key = key, ties = want;
         // what the first k weigh: above the bin, and the listed tokens above the cut (or the row's tokens above it)
-        double w = in_lds && tid < bin ? sh.bin_weight[tid] : 0.0;
+        double w = in_lds && tid == 0 && bin ? sh.upto_weight[bin - 1] : 0.0;
         for (int i = from; i < end; i += step) {
           const unsigned k = key_at(i);
           if (k > key) w += (double)row_weight(k);
@@ -566,16 +598,9 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
           if (k > t_key || (k == t_key && x <= last)) atomicAdd(&sh.inside[x / kStretch], row_weight(k));
         }
         __syncthreads();
-#pragma unroll 1
-        for (int i = wave; i < NS; i += kRowWaves) {
-          double m = 0;
-#pragma unroll
-          for (int j = 0; j < kLogitBins; j += 64) {
-            const double x = ws.bin_weight[(at0 + i) * kLogitBins + j + lane];
-            m += j + lane < bin - sh.below[i] ? x : 0.0;
-          }
-          m = wave_scan(m);
-          if (lane == 63) sh.kept[i] = m * sh.scale[i] + (double)sh.inside[i];
+        if (tid < NS) {
+          const int j = min(bin - sh.below[tid], kLogitBins) - 1;  // the last bin before it
+          sh.kept[tid] = (j >= 0 ? ws.upto_weight[(at0 + tid) * kLogitBins + j] * sh.scale[tid] : 0.0) + (double)sh.inside[tid];
         }
       } else {
 #pragma unroll 1
@@ -626,7 +651,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
 #pragma unroll
   for (int i = 0; i < TPT; ++i) {
     const unsigned k = usable(v[i]) ? order_key(v[i]) : 0;
-    w[i] = k && (k > t_key || (k == t_key && (unsigned)(first + tid * TPT + i) <= last)) ? fixed_of(weight_of(v[i], local, per_t, powers)) : 0;
+    w[i] = k && (k > t_key || (k == t_key && (unsigned)(first + tid * TPT + i) <= last)) ? ex.fixed(v[i], local, per_t) : 0;
     sum += w[i];
   }
   u64 whole_stretch, before = block_scan(sum, sh, lane, wave, whole_stretch) - sum;
@@ -640,7 +665,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
       a.token[b] = first + tid * TPT + i;
       if (a.logprob) {
         // log of the sum: a logarithm in 32 bits and what the exponential in 64 leaves of it
-        const double sum1 = all / kOne, y = (double)logf((float)sum1), r = sum1 * exp2_32nds(-y * kPerT, powers) - 1.0;
+        const double sum1 = all / kOne, y = (double)logf((float)sum1), r = sum1 * ex.at(-y * kPerT) - 1.0;
         a.logprob[b] = (float)(((double)v[i] - (double)top) * per_t / kPerT - y - (r - 0.5 * r * r));
       }
     }
@@ -663,11 +688,11 @@ SampleLayout sample_layout(int batch, int vocab, void* base) {
     l.bytes += al(bytes);
     return q;
   };
-  l.ws.bin_weight = reinterpret_cast<double*>(take(n * kLogitBins * 8));
+  l.ws.upto_weight = reinterpret_cast<double*>(take(n * kLogitBins * 8));
   l.ws.weight = reinterpret_cast<double*>(take(n * 8));
   l.ws.top = reinterpret_cast<float*>(take(n * 4));
   l.ws.usable = reinterpret_cast<unsigned*>(take(n * 4));
-  l.ws.bin_count = reinterpret_cast<unsigned short*>(take(n * kLogitBins * 2));
+  l.ws.upto_count = reinterpret_cast<unsigned short*>(take(n * kLogitBins * 2));
   return l;
 }
 
@@ -711,8 +736,8 @@ extern "C" harli_status harli_sample(const harli_sample_batch* b, void* hip_stre
   if (rc != HARLI_OK) return rc;
   const SampleWs ws = sample_layout(b->batch, b->vocab, b->workspace).ws;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  hipLaunchKernelGGL(k_sample_stretch, dim3(ws.n, b->batch), dim3(kStretchThreads), 0, st, *b, ws);
-  hipLaunchKernelGGL(k_sample_row, dim3(b->batch), dim3(kRowThreads), sizeof(RowShared), st, *b, ws);
+  hipLaunchKernelGGL(k_sample_stretch, dim3(ws.n, b->batch), dim3(kStretchThreads), 0, st, *b, ws, kSeries);
+  hipLaunchKernelGGL(k_sample_row, dim3(b->batch), dim3(kRowThreads), sizeof(RowShared), st, *b, ws, kSeries);
   HARLI_HIP(hipGetLastError());
   return HARLI_OK;
 }
