@@ -21,14 +21,14 @@ namespace harli {
 namespace {
 
 typedef unsigned long long u64;
-constexpr int kStretch = 4096;      // tokens per workgroup of the first launch: sixteen per thread
-constexpr int kMostVocab = 1 << 20;  // 256 stretches
+constexpr int kStretch = 4096;      // tokens per workgroup of the first launch: 16 per thread
+constexpr int kMostVocab = 1 << 20;
 constexpr int kMostStretches = kMostVocab / kStretch;
 constexpr int kLogitBins = 256;     // of a stretch, downwards from its maximum
 constexpr int kCandidates = 8192;   // tokens of one bin that the second launch holds in LDS
 constexpr int kDigits = 2048;       // bins of a search: 11 bits
 constexpr int kRowThreads = 1024, kRowWaves = kRowThreads / 64;
-constexpr double kOne = (double)(1ull << 50);  // weight 1 in fixed point: 2^12 of them and more fit 64 bits
+constexpr double kOne = (double)(1ull << 50);  // weight 1 in fixed point: 2^13 of them fit 64 bits
 
 // Order of the logits as unsigned integers; both zeros alike.
 __device__ __forceinline__ unsigned order_key(float v) {
@@ -47,47 +47,56 @@ constexpr double exp_series(double x) {
   return sum;
 }
 struct Powers {
-  double v[kPowersN];
+  double v[kPowersN], down[kPowersN];  // 2^(j / 64), 2^(-j / 64)
 };
 constexpr Powers make_powers() {
   Powers t{};
-  for (int j = 0; j < kPowersN; ++j) t.v[j] = exp_series(kLn2 * j / kPowersN);
+  for (int j = 0; j < kPowersN; ++j) t.v[j] = exp_series(kLn2 * j / kPowersN), t.down[j] = exp_series(-kLn2 * j / kPowersN);
   return t;
 }
 __constant__ Powers kPowers = make_powers();
 
-// 2^(t / 64): t = 64 e + j + f; the table's 2^(j / 64) times the series of exp(f ln 2 / 64) over |f| <= 1/2 to the fourth power (what
-// follows is below 2^-44).  The coefficients come as kernel arguments, that is as scalar operands: as immediates every one of them
-// is moved into registers for every token.
+// 2^((n + f) / 64), n a whole number, |f| <= 1/2: n = 64 e + j; the table's 2^(j / 64) times the series of exp(f ln 2 / 64) to the fourth
+// power (what follows is below 2^-44).  The coefficients come as kernel arguments, that is as scalar operands: as immediates every one
+// of them is moved into registers for every token.
 struct Series {
-  double c1, c2, c3, c4, two52;
+  double c1, c2, c3, c4;
 };
 constexpr Series kSeries = {kLn2 / 64, kLn2 / 64 * (kLn2 / 64) / 2, kLn2 / 64 * (kLn2 / 64) * (kLn2 / 64) / 6,
-                            kLn2 / 64 * (kLn2 / 64) * (kLn2 / 64) * (kLn2 / 64) / 24, (double)(1ull << 52)};
+                            kLn2 / 64 * (kLn2 / 64) * (kLn2 / 64) * (kLn2 / 64) / 24};
 struct Exp {
   Series s;
   const double* powers;  // the table in LDS
-  __device__ __forceinline__ double at(double t) const {
-    const double n = rint(t), f = t - n;
-    const int i = (int)n;  // (far below the range it saturates: zero)
+  __device__ __forceinline__ double at(int n, double f) const {
     const double p = fma(fma(fma(fma(s.c4, f, s.c3), f, s.c2), f, s.c1), f, 1.0);
-    return __builtin_amdgcn_ldexp(p * powers[i & (kPowersN - 1)], i >> 6);
+    return __builtin_amdgcn_ldexp(p * powers[n & (kPowersN - 1)], n >> 6);
+  }
+  __device__ __forceinline__ double at(double t) const {
+    const double n = rint(t);
+    return at((int)n, t - n);  // (far below the range it saturates: zero)
   }
   // weight of a usable logit relative to `top`, which is not infinite; per_t = 64 log2(e) / temperature
   __device__ __forceinline__ double weight(float v, float top, double per_t) const { return at(((double)v - (double)top) * per_t); }
-  // ... in fixed point: added to 2^52, the integer part of w * kOne stands in the low bits, rounded (w <= 1)
-  __device__ __forceinline__ u64 fixed(float v, float top, double per_t) const {
-    return (u64)__double_as_longlong(fma(weight(v, top, per_t), kOne, s.two52)) & ((1ull << 52) - 1);
-  }
+  __device__ __forceinline__ u64 fixed(float v, float top, double per_t) const { return fixed_of(weight(v, top, per_t)); }
+  // kOne stands for 1 (and w <= 1): beside 4 the last bit of a number is 2^-50
+  static __device__ __forceinline__ u64 fixed_of(double w) { return (u64)__double_as_longlong(w + 4.0) & ((1ull << 52) - 1); }
 };
 // A row with logits of +inf is one of them alone, at zero.
 __device__ __forceinline__ float finite_row(float v) { return v == INFINITY ? 0.f : -INFINITY; }
-// Bins of the logit for a row: their width is an eighth of the temperature, within 1/16 and 1/8 of the logit's unit, so that 256 of them span 16
-// units at least and one holds a few per cent of a vocabulary at most.  They lie on a grid common to all stretches.
-__device__ __forceinline__ float bins_per_unit(float t) { return fminf(fmaxf(8.f / t, 8.f), 16.f); }
-__device__ __forceinline__ int bin_of(float v, float per_unit) {  // monotone; kept inside the integers
-  return (int)floorf(__builtin_amdgcn_fmed3f(v * per_unit, -5e8f, 5e8f));
+// Where a logit lies, in 64ths of a power of two of its weight: v * per_t, rounded to a whole number.  A bin is 2^shift of them, on a grid
+// common to all stretches: an eighth to a sixteenth of the logit's unit, so that 256 bins span 16 units at least and one holds a
+// few per cent of a vocabulary at most (bins are wider above a temperature of 5, and span less below one of 1/22).
+__device__ __forceinline__ int bin_shift(float t) { return max(1, min(7, ilogbf(11.54f / t))); }  // 2^shift * t ln(2) / 64 <= 1/8
+// Beside 3 * 2^51 the last bit of a number is 1, also with an even number added: what a sum there rounds to does not depend on the latter.
+constexpr double kWholes = 3.0 * (double)(1ull << 51);
+__device__ __forceinline__ double whole_of(float v, double per_t) { return fma((double)v, per_t, kWholes) - kWholes; }
+// the border of the grid at or above it
+__device__ __forceinline__ double ceiling_of(float top, double per_t, int shift) {
+  return __builtin_amdgcn_ldexp(ceil(__builtin_amdgcn_ldexp(whole_of(top, per_t), -shift)), shift);
 }
+// Whole numbers are exact below 2^53.  A row whose largest logit is further away than 2^43 is searched and summed up by its differences
+// from that logit; a stretch whose largest is further than 2^44 weighs nothing in any other row.
+constexpr double kFarRow = (double)(1ull << 43), kFarStretch = (double)(1ull << 44);
 
 constexpr double kPerT = 64 * 1.4426950408889634074;
 struct RowSettings {
@@ -193,7 +202,7 @@ __global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample
   }
   const RowSettings s = settings_of(a, b);
   bin_weight[tid] = 0, bin_count[tid] = 0;
-  if (tid < kPowersN) powers[tid] = kPowers.v[tid];
+  if (tid < kPowersN) powers[tid] = kPowers.down[tid];
   float top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) top = fmaxf(top, v[i]);  // (NaN is the other operand)
@@ -204,29 +213,58 @@ __global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample
   const size_t at = (size_t)b * ws.n + blockIdx.x;
   if (tid == 0) ws.top[at] = top;
   if (s.greedy) return;
-  if (top == INFINITY) {  // (the bins of such a row: its tokens of +inf in the first, like the row's)
+  const bool infinite = top == INFINITY;
+  if (infinite) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) v[i] = finite_row(v[i]);
     top = 0.f;
   }
   const double per_t = kPerT / (double)s.t;
-  const Exp ex{series, powers};
-  const float per_unit = bins_per_unit(s.t);
-  const int bin0 = bin_of(top, per_unit);
+  const int shift = bin_shift(s.t);
+  const double ceiling = ceiling_of(top, per_t, shift);
+  const bool far = !(fabs(ceiling) < kFarStretch);
   u64 sum = 0;
   unsigned count = 0;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const bool in = usable(v[i]);
-    const u64 w = in ? ex.fixed(v[i], top, per_t) : 0;
+  // Logits below the bins and below all weights (2^-60) are taken as the one at that border.  This is the loop that the launch's time
+  // goes into: conversions between 64-bit floating point and integers, and ldexp, are slow beside sums and products, hence the sums beside
+  // kWholes and the exponent added as bits.
+  const double border = (ceiling - (double)(max(60 * 64, kLogitBins << shift) + 64)) / per_t;
+  const float least = border > -3e38 ? (float)border : -INFINITY;
+  const double wholes = kWholes + ceiling;
+  double c3 = series.c3;
+  asm("" : "+v"(c3));  // (one scalar operand per instruction)
+  auto add = [&](float x, bool masked) {
+    x = __builtin_amdgcn_fmed3f(x, least, INFINITY);  // (least for NaN too)
+    const double d = (double)x, y = fma(d, -per_t, wholes), f = fma(d, per_t, y - wholes);
+    const unsigned below = (unsigned)(u64)__double_as_longlong(y);  // wholes below the ceiling
+    const double p = fma(fma(fma(fma(series.c4, f, c3), f, series.c2), f, series.c1), f, 1.0) * powers[below & (kPowersN - 1)];
+    u64 w = Exp::fixed_of(__hiloint2double(__double2hiint(p) - (int)((below << 14) & 0xfff00000u), __double2loint(p)));
+    if (masked && x == -INFINITY) w = 0;
     sum += w;
-    count += in;
     if (s.cut) {
-      const int bin = bin0 - bin_of(v[i], per_unit);
-      if (in && bin < kLogitBins) atomicAdd(&bin_weight[bin], w);
-      if (s.k && in && bin < kLogitBins) atomicAdd(&bin_count[bin], 1u);
+      const unsigned bin = below >> shift;
+      if (bin < kLogitBins && !(masked && x == -INFINITY)) {
+        atomicAdd(&bin_weight[bin], w);
+        if (s.k) atomicAdd(&bin_count[bin], 1u);
+      }
     }
+  };
+  if (least > -INFINITY) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) add(v[i], false);
+  } else {  // a temperature at which no logit is too small
+#pragma unroll 1
+    for (int i = 0; i < kStretch; i += kStretchThreads)
+      if (i + tid < n) {
+        const float x = z[i + tid];
+        add(infinite ? finite_row(x) : x, true);
+      }
   }
+  if (s.k) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) count += usable(v[i]);
+  }
+  if (far) sum = 0;
   sum = wave_scan(sum);
   count = wave_scan(count);
   if (lane == 63) s_weight[wave] = sum, s_n[wave] = count;
@@ -237,8 +275,8 @@ __global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample
   }
   if (s.cut) {
     static_assert(kLogitBins == kStretchThreads, "a bin per thread");
-    u64 w = wave_scan(bin_weight[tid]);
-    unsigned c = wave_scan(bin_count[tid]);
+    u64 w = wave_scan(far ? 0 : bin_weight[tid]);
+    unsigned c = wave_scan(far ? 0 : bin_count[tid]);
     __syncthreads();
     if (lane == 63) s_weight[wave] = w, s_n[wave] = c;
     __syncthreads();
@@ -253,7 +291,6 @@ __global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample
 // cold.  The three searches (for top-k, for top-p, for the last of equal logits) are therefore one loop around one search.
 constexpr int kPart = 1024;                        // tokens that a wave looks through at a time for those of a bin
 constexpr int kListed = kCandidates / kRowWaves;   // tokens of the bin a wave can hold: every wave has a list of its own
-constexpr float kExactBins = (float)(1 << 22);     // bins up to here are told apart by comparing with their borders
 
 struct RowShared {
   u64 digit[kDigits];
@@ -261,7 +298,7 @@ struct RowShared {
   unsigned key[kCandidates], index[kCandidates];
   float top[kMostStretches];
   int below[kMostStretches];      // bins from the row's first to the stretch's
-  double scale[kMostStretches];   // weight of the stretch's largest logit in the row
+  double scale[kMostStretches];   // of the stretch's sums to the row's, which are relative to its largest logit
   double kept[kMostStretches];
   u64 inside[kMostStretches];     // kept weight of the cut's own bin, in the row's fixed point
   double upto_weight[kLogitBins];  // of the row's bins up to each one
@@ -343,6 +380,23 @@ __device__ __forceinline__ unsigned find_key(int from, int end, int step, unsign
   return prefix;
 }
 
+// The smallest key that `enough` holds for, which it does from some key up to `hi` (and not for keys of NaN): 64 keys at a time, first those
+// around a guess.  A wave's work, the same in all of them.
+template <typename Enough>
+__device__ __forceinline__ unsigned smallest_key(Enough enough, float guess, unsigned hi, int lane) {
+  unsigned lo = 0, step = 1, at = order_key(guess) - 33;  // keys at + step * (1, 2, .. 64)
+#pragma unroll 1
+  while (true) {
+    const u64 k = (u64)at + (u64)step * (lane + 1);
+    const u64 m = __ballot(k >= hi || enough((unsigned)k));
+    const int i = m ? __ffsll(m) - 1 : 64;
+    if (i < 64) hi = min(hi, at + step * (i + 1));
+    if (i > 0) lo = max(lo, at + step * i);
+    if (hi - lo <= 1) return hi;
+    step = (hi - lo + 63) / 64, at = lo;
+  }
+}
+
 __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a, SampleWs ws, Series series) {
   extern __shared__ __align__(16) char row_lds[];
   RowShared& sh = *reinterpret_cast<RowShared*>(row_lds);
@@ -384,14 +438,20 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
   if (infinite) mine = finite_row(mine), top = 0.f;
   const double per_t = kPerT / (double)s.t;
   const Exp ex{series, sh.powers};
-  const float per_unit = bins_per_unit(s.t);
-  const int bin0 = bin_of(top, per_unit);
+  const int shift = bin_shift(s.t);
+  const double ceiling = ceiling_of(top, per_t, shift);
+  const bool far = !(fabs(ceiling) < kFarRow);  // uniform
+  auto bin_of = [&](unsigned key) {             // of the row
+    const double n = __builtin_amdgcn_ldexp(ceiling - whole_of(order_value(key), per_t), -shift);
+    return n < (double)kLogitBins ? (int)n : kLogitBins;  // (keys of NaN: none)
+  };
   double whole_mine = 0;
   if (tid < NS) {
-    const bool some = usable(mine);
-    const double scale = some ? ex.weight(mine, top, per_t) : 0.0;
+    const bool some = usable(mine) && !far;
+    const double own = ceiling_of(mine, per_t, shift), steps = __builtin_amdgcn_ldexp(ceiling - own, -shift);
+    const double scale = some ? ex.at(fma(-(double)top, per_t, own)) : 0.0;  // of the stretch's sums, which are relative to its ceiling
     sh.top[tid] = mine;
-    sh.below[tid] = some ? bin0 - bin_of(mine, per_unit) : kLogitBins;
+    sh.below[tid] = some && steps < (double)kLogitBins ? (int)steps : kLogitBins;
     sh.scale[tid] = scale;
     whole_mine = some ? ws.weight[at0 + tid] * scale : 0.0;
     sh.kept[tid] = whole_mine;
@@ -400,7 +460,14 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
 
   // ---- the cut: logits with keys above t_key stay, and of those equal to it the ones up to index last ----------------------------
   unsigned t_key = 0, last = 0xffffffffu;
+  int held = -1;  // the bin whose tokens are in LDS, and this wave's number of them
+  int listed = 0;
+  bool in_lds = false;
   if (s.cut) {
+    if (far) {
+      for (int i = tid; i < V; i += kRowThreads)
+        if (usable(logit(i))) whole_mine += (double)row_weight(order_key(logit(i)));
+    }
     double among = all_sum(whole_mine, sh, lane, wave);  // weight of the tokens that top-k leaves, in the row's fixed point
     {  // bins of the row
       constexpr int NG = kRowThreads / kLogitBins;
@@ -427,9 +494,6 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
       __syncthreads();
     }
     u64 ties = ~0ull;  // how many of the tokens equal to t_key stay
-    int held = -1;     // the bin whose tokens are in LDS, and this wave's number of them
-    int listed = 0;
-    bool in_lds = false;
 #pragma unroll 1
     for (int phase = 0; phase < 3; ++phase) {
       int bin = kLogitBins;  // that the phase looks into; kLogitBins: none of them, it looks through the row
@@ -456,25 +520,14 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
         bin = sh.found;
             } else {  // the cut's own bin, for the last of equal logits and for the weights
         if (s.min_p > 0.0) {
-          // the smallest key whose weight is min_p or more: 64 keys at a time, the same search in every wave
-          unsigned lo = 0, hi = order_key(top);  // lo: too small, hi: large enough
-#pragma unroll 1
-          while (hi - lo > 1) {
-            const unsigned step = (hi - lo + 63) / 64;
-            const u64 k = (u64)lo + (u64)step * (lane + 1);
-            const bool enough = k >= hi || ex.weight(order_value((unsigned)k), top, per_t) >= s.min_p;  // (keys of NaN weigh nothing)
-            const int i = __ffsll(__ballot(enough)) - 1;  // the last lane is past hi
-            const u64 next = (u64)lo + (u64)step * (i + 1);
-            lo += step * i;
-            hi = next < hi ? (unsigned)next : hi;
-          }
+          const unsigned hi = smallest_key([&](unsigned k) { return ex.weight(order_value(k), top, per_t) >= s.min_p; },
+                                           top + s.t * logf((float)s.min_p), order_key(top), lane);
           if (hi > t_key) t_key = hi, ties = ~0ull;
         }
         if (!t_key) break;
-        bin = bin0 - bin_of(order_value(t_key), per_unit);
+        bin = bin_of(t_key);
       }
-      const float border = (float)(bin0 - bin);
-      if (!(fabsf(border) < kExactBins)) bin = kLogitBins;
+      if (far) bin = kLogitBins;
 
       // ---- the tokens of the bin, in LDS (their order there is of no account)
       if (bin < kLogitBins && bin != held) {
@@ -490,6 +543,12 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
           sh.some[tid] = some;
         }
         __syncthreads();
+        // the logits of the bin: from the smallest in it (or above) to the smallest above it
+        float border[2];
+#pragma unroll 1
+        for (int above = 0; above < 2; ++above)
+          border[above] = order_value(smallest_key([&](unsigned k) { return bin_of(k) <= bin - above; },
+                                                   (float)((ceiling + 0.5 - (double)((bin + 1 - above) << shift)) / per_t), order_key(INFINITY), lane));
         // the next part's tokens are in flight while this part's are looked at
         constexpr int R = kPart / 64;
         auto needed = [&](int lo) {
@@ -513,8 +572,8 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
 #pragma unroll
           for (int r = 0; r < R; ++r) {
             const int x = now + r * 64 + lane;
-            const float f = infinite ? finite_row(v[r]) : v[r], scaled = f * per_unit;
-            const bool in = scaled >= border && scaled < border + 1.f && x < V;
+            const float f = infinite ? finite_row(v[r]) : v[r];
+            const bool in = f >= border[0] && f < border[1] && x < V;
             const u64 who = __ballot(in);
             if (who) {
               const int at = listed + (int)__popcll(who & ((1ull << lane) - 1));
@@ -586,7 +645,10 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
         last = (unsigned)(kMostVocab - 1) - key;
       }
     }
-    // kept weight of every stretch
+  }
+  if (far && !t_key) t_key = 1;  // (below every key: nothing is cut off)
+  // kept weight of every stretch
+  {
     if (t_key) {
       __syncthreads();
       if (in_lds) {
@@ -655,7 +717,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
     sum += w[i];
   }
   u64 whole_stretch, before = block_scan(sum, sh, lane, wave, whole_stretch) - sum;
-  const double x = offset / sh.scale[pick];
+  const double x = offset / ex.weight(local, top, per_t);
   u64 target = x >= (double)whole_stretch ? whole_stretch - 1 : x > 0 ? (u64)x : 0;
   if (target >= whole_stretch) target = whole_stretch - 1;
   if (target < before || target >= before + sum) return;
