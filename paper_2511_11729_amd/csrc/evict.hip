@@ -3,17 +3,22 @@
 // Reads 8 bytes per token and moves whole rows of keys and values: bound by HBM.  Only rows behind the kept length move (not
 // everything behind the first gap, as keeping the order would): a service that gives up one page of 16 tokens at a time moves at
 // most 16 rows per head, and sources (slots >= keep) and targets (slots < keep) never meet, so rows move in any order.
+#include <algorithm>
+#include <mutex>
+
 #include "ctx.h"
 #include "device_utils.h"
+#include "scan_utils.h"
 
 namespace harli {
 namespace {
 
 constexpr int kPageTokens = 16;
 constexpr int kMostPages = 1 << 26;  // of a table row: token indexes stay in 32 bits
-constexpr int kMoves = 1024;          // moves listed in LDS at a time
+constexpr int kMoves = 512;           // moves listed in LDS at a time
 constexpr int kMostTokens = 1 << 18;  // of a sequence: a bit each in LDS
 constexpr int kBins = 2048;           // of the search for the last weight that stays: 11, 11 and 10 bits
+constexpr int kKeysInLds = 32768;     // tokens whose keys are read once and stay in LDS; of longer sequences they are read again for every pass
 
 // Order of the weights as unsigned integers: NaN below every other, both zeros alike, protected tokens above.
 __device__ __forceinline__ unsigned rank_key(uint2 rec, int sink, long long recent_from) {
@@ -27,45 +32,49 @@ __device__ __forceinline__ unsigned rank_key(uint2 rec, int sink, long long rece
 // Sum of v over the threads before this one, and of all of them in `all` (the whole workgroup calls it; `tmp`: one entry per wave).
 template <int NW>
 __device__ __forceinline__ int scan_before(int v, int* tmp, int lane, int wave, int& all) {
-  int s = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int x = __shfl_up(s, o, 64);
-    if (lane >= o) s += x;
-  }
+  const int s = wave_scan(v);
   __syncthreads();  // tmp is free
   if (lane == 63) tmp[wave] = s;
   __syncthreads();
-  int before = 0;
-  all = 0;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    if (w < wave) before += tmp[w];
-    all += tmp[w];
-  }
-  return before + s - v;
+  const int t = row_scan(lane < NW ? tmp[lane] : 0);
+  all = lane_value(t, NW - 1);
+  const int before = lane_value(t, wave ? wave - 1 : 0);
+  return (wave ? before : 0) + s - v;
 }
 
 struct EvictArgs {
   harli_evict_batch b;
-  int n_kv, row_bytes;
+  int n_kv, row_bytes, row_lanes;  // row_lanes: the power of two of lanes that move a row, words of it each
+  int parts;                       // workgroups per (layer, sequence, KV head): each moves rows of its own
+  bool rows, records;              // what this launch moves
   char* slab;
   KvGeom geom;
   int* err_flag;
 };
 
-// NT threads with KR keys each in registers (KR = 0: keys are read again for every pass); rows move in words of VEC bytes.
-// A wave's 64 keys of one round are 64 tokens in a row: their ballot is a word of the bitmap of those that stay.
-template <int NT, int KR, int VEC>
+// LDS: a bit per token that stays, then keys and bins of the search, whose place the moves' offsets take afterwards.
+struct Move {
+  unsigned long long src, dst;  // of a key's row, from the slab's start
+};
+size_t evict_lds(int max_kv_len, bool keys) {
+  const size_t bits = ((size_t)max_kv_len + 63) / 64 * 8, search = (keys ? ((size_t)max_kv_len + 3) / 4 * 16 : 0) + kBins * 4;
+  return bits + std::max(search, (size_t)kMoves * (sizeof(Move) + 8)) + 16;
+}
+
+// NT threads; KEYS: the keys stay in LDS; rows move in words of VEC bytes.
+// The time goes into the rows at large sizes, and into latencies and the kernel's own code at small ones, hence loops instead of unrolled
+// rounds over keys in registers (39 KB of code: 21.6 us for 16 sequences that give up one page of 1040 tokens in eight layers).
+template <int NT, bool KEYS, int VEC>
 __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
   constexpr int NW = NT / 64, BPT = kBins / NT;
-  static_assert(kBins % NT == 0, "whole bins per thread");
+  static_assert(kBins % NT == 0 && NW <= 16, "whole bins per thread; the waves' sums in a row of lanes");
   const harli_evict_batch& a = args.b;
   const KvGeom& geom = args.geom;
   const int n_kv = args.n_kv;
-  const int c = blockIdx.x, b = blockIdx.y, layer = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int c = blockIdx.x / args.parts, part = blockIdx.x - c * args.parts, b = blockIdx.y, layer = blockIdx.z;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = a.n_tokens[b], keep = max(a.keep[b], 0);
-  const bool first = c == 0 && layer == 0;
+  const bool first = c == 0 && layer == 0 && part == 0;
   if (n > a.max_kv_len || n > a.max_pages * kPageTokens) {
     if (first && tid == 0) {
       atomicOr(args.err_flag, 4);
@@ -80,59 +89,48 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
   harli_kv_record* rec = a.records + ((size_t)layer * geom.n_pages_total * n_kv + c) * kPageTokens;
   const size_t page_recs = (size_t)n_kv * kPageTokens;
   auto good = [&](int page) { return page >= 0 && page < geom.n_pages_total; };
+
+  extern __shared__ __align__(16) char evict_lds_mem[];
+  u64* stays = reinterpret_cast<u64*>(evict_lds_mem);  // a bit per token
+  char* rest = evict_lds_mem + (((size_t)a.max_kv_len + 63) / 64 * 8 + 15) / 16 * 16;
+  int* hist = reinterpret_cast<int*>(rest);
+  unsigned* keys = reinterpret_cast<unsigned*>(rest + kBins * 4);
+  Move* moves = reinterpret_cast<Move*>(rest);  // once the search is done
+  int2* pairs = reinterpret_cast<int2*>(rest + kMoves * sizeof(Move));
+  __shared__ int tmp[NW], s_bin, s_above, s_count;
+
   auto load_key = [&](int t) -> unsigned {  // of a token of the sequence
     const int page = table[t / kPageTokens];
-    if (!good(page)) {
-      if (first) atomicOr(args.err_flag, 1);
-      return 0;
-    }
-    return rank_key(*reinterpret_cast<const uint2*>(rec + page * page_recs + t % kPageTokens), a.sink, recent_from);
+    const bool ok = good(page);
+    if (!ok && first) atomicOr(args.err_flag, 1);
+    const uint2 r = *reinterpret_cast<const uint2*>(rec + (ok ? page : 0) * page_recs + t % kPageTokens);
+    return ok ? rank_key(r, a.sink, recent_from) : 0;
   };
-
-  extern __shared__ unsigned long long stays[];  // a bit per token
-  __shared__ int hist[kBins], tmp[NW], s_bin, s_above, s_count;
-  __shared__ int from[kMoves], to[kMoves];
-
-  unsigned key[KR ? KR : 1];
-  const int rounds = (n + NT - 1) / NT;
-  if constexpr (KR > 0) {
-#pragma unroll
-    for (int i = 0; i < KR; ++i) {
-      const int t = i * NT + tid;
-      key[i] = 0;
-      if (i < rounds && t < n) key[i] = load_key(t);
-    }
-  }
-  // f(round, token, key) for the rounds of this thread; token >= n: none (key 0)
-  auto each = [&](auto&& f) {
-    if constexpr (KR > 0) {
-#pragma unroll
-      for (int i = 0; i < KR; ++i)
-        if (i < rounds) f(i * NT + tid, key[i]);
-    } else {
+  if constexpr (KEYS) {
 #pragma unroll 4
-      for (int i = 0; i < rounds; ++i) {
-        const int t = i * NT + tid;
-        f(t, t < n ? load_key(t) : 0u);
-      }
-    }
-  };
+    for (int t = tid; t < n; t += NT) keys[t] = load_key(t);
+  }
+  auto key_of = [&](int t) { return KEYS ? keys[t] : load_key(t); };
 
   // ---- the keep-th largest key, digit by digit: a token stays if its key is above `prefix`, or equal to it (in the digits seen)
   // and among the first `want` of those ------------------------------------------------------------------------------------
   unsigned prefix = 0, mask = 0;
   int want = keep, count = n;
+#pragma unroll 1
   for (int shift = 21; keep > 0 && want < count && shift >= 0; shift = shift == 21 ? 10 : shift == 10 ? 0 : -1) {
     const unsigned digits = shift ? 2047u : 1023u;
-    for (int i = tid; i < kBins; i += NT) hist[i] = 0;
-    __syncthreads();
-    each([&](int t, unsigned k) {
-      if (t < n && (k & mask) == prefix) atomicAdd(&hist[(k >> shift) & digits], 1);
-    });
-    __syncthreads();
-    int h[BPT], sum = 0, all;  // thread 0 has the highest bins
 #pragma unroll
-    for (int i = 0; i < BPT; ++i) h[i] = hist[kBins - 1 - (tid * BPT + i)], sum += h[i];
+    for (int i = 0; i < BPT; ++i) hist[tid * BPT + i] = 0;
+    __syncthreads();
+#pragma unroll 4
+    for (int t = tid; t < n; t += NT) {
+      const unsigned k = key_of(t);
+      if ((k & mask) == prefix) atomicAdd(&hist[kBins - 1 - ((k >> shift) & digits)], 1);  // the highest first
+    }
+    __syncthreads();
+    int h[BPT], sum = 0, all;
+#pragma unroll
+    for (int i = 0; i < BPT; ++i) h[i] = hist[tid * BPT + i], sum += h[i];
     int above = scan_before<NW>(sum, tmp, lane, wave, all);
     if (above < want && above + sum >= want) {
 #pragma unroll
@@ -146,37 +144,30 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
     count = s_count;
     prefix |= (unsigned)s_bin << shift;
     mask |= digits << shift;
-    __syncthreads();
   }
+  __syncthreads();
 
-  // ---- who stays ---------------------------------------------------------------------------------------------------------
-  if (keep == 0) {
-    for (int i = tid; i < (n + 63) / 64; i += NT) stays[i] = 0;
-  } else if (want == count) {  // all of the last ones
-    each([&](int t, unsigned k) {
-      const unsigned long long m = __ballot(t < n && (k & mask) >= prefix);
-      if (lane == 0 && t < n) stays[t / 64] = m;
-    });
-  } else {  // equal keys: the first `want` of them, in order of the slots
-    int seen = 0;
-    each([&](int t, unsigned k) {
+  // ---- who stays: 64 tokens in a row are a ballot ---------------------------------------------------------------------------
+  int seen = 0;  // equal keys before the tokens at hand; of them, in order of the slots, the first `want` stay
+  const bool all_equal = want == count;
+#pragma unroll 1
+  for (int t0 = 0; t0 < n; t0 += NT) {
+    const int t = t0 + tid;
+    const unsigned k = t < n && keep > 0 ? key_of(t) : 0;
+    bool in = t < n && keep > 0 && (k & mask) >= prefix;
+    if (!all_equal && keep > 0) {
       const bool eq = t < n && k == prefix;
-      const unsigned long long me = __ballot(eq);
-      int all;
+      const u64 me = __ballot(eq);
       __syncthreads();
       if (lane == 0) tmp[wave] = __popcll(me);
       __syncthreads();
-      int r = seen + __popcll(me & ((1ull << lane) - 1));
-      all = 0;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        if (w < wave) r += tmp[w];
-        all += tmp[w];
-      }
-      seen += all;
-      const unsigned long long m = __ballot(t < n && (k > prefix || (eq && r < want)));
-      if (lane == 0 && t < n) stays[t / 64] = m;
-    });
+      const int sums = row_scan(lane < NW ? tmp[lane] : 0);
+      const int before = lane_value(sums, wave ? wave - 1 : 0);
+      if (eq) in = seen + (wave ? before : 0) + (int)__popcll(me & ((1ull << lane) - 1)) < want;
+      seen += lane_value(sums, NW - 1);
+    }
+    const u64 m = __ballot(in);
+    if (lane == 0 && t < n) stays[t / 64] = m;
   }
   __syncthreads();
 
@@ -188,41 +179,108 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
   int holes = 0, movers = 0, total, total_movers;
   for (int w = w_lo; w < w_hi; ++w) holes += __popcll(holes_of(w)), movers += __popcll(movers_of(w));
   const int h0 = scan_before<NW>(holes, tmp, lane, wave, total), m0 = scan_before<NW>(movers, tmp, lane, wave, total_movers);
-  const int row_words = args.row_bytes / VEC;
   typedef unsigned int __attribute__((ext_vector_type(VEC / 4))) word;
-  for (int first_move = 0; first_move < total; first_move += kMoves) {
-    int h = h0 - first_move, m = m0 - first_move;
+  const int row_words = args.row_bytes / VEC, row_lanes = args.row_lanes, per_pass = NT / row_lanes, x0 = tid & (row_lanes - 1), r0 = tid / row_lanes;
+  const int share = (total + args.parts - 1) / args.parts, end = min(total, (part + 1) * share);
+#pragma unroll 1
+  for (int at = part * share; at < end; at += kMoves) {
+    __syncthreads();
+    int h = h0 - at, m = m0 - at;
     for (int w = w_lo; w < w_hi; ++w) {
-      for (unsigned long long x = holes_of(w); x; x &= x - 1, ++h)
-        if (h >= 0 && h < kMoves) to[h] = 64 * w + __ffsll(x) - 1;
-      for (unsigned long long x = movers_of(w); x; x &= x - 1, ++m)
-        if (m >= 0 && m < kMoves) from[m] = 64 * w + __ffsll(x) - 1;
+      const u64 hs = holes_of(w), ms = movers_of(w);
+      if (h < kMoves && h + (int)__popcll(hs) > 0)
+        for (u64 x = hs, i = h; x; x &= x - 1, ++i)
+          if ((int)i >= 0 && (int)i < kMoves) pairs[i].y = 64 * w + __ffsll(x) - 1;
+      if (m < kMoves && m + (int)__popcll(ms) > 0)
+        for (u64 x = ms, i = m; x; x &= x - 1, ++i)
+          if ((int)i >= 0 && (int)i < kMoves) pairs[i].x = 64 * w + __ffsll(x) - 1;
+      h += __popcll(hs), m += __popcll(ms);
     }
     __syncthreads();
-    const int moves = min(kMoves, total - first_move);
-#pragma unroll 4
-    for (int i = tid; i < moves * 2 * row_words; i += NT) {
-      const int r = i / row_words, x = i - r * row_words, src = from[r >> 1], dst = to[r >> 1], ps = table[src / kPageTokens], pd = table[dst / kPageTokens];
-      if (!good(ps) || !good(pd)) continue;
-      const size_t head = (size_t)c * kPageTokens;
-      const word v = *reinterpret_cast<const word*>(args.slab + kv_page_off(geom, ps, layer, r & 1) + (head + src % kPageTokens) * args.row_bytes + x * VEC);
-      *reinterpret_cast<word*>(args.slab + kv_page_off(geom, pd, layer, r & 1) + (head + dst % kPageTokens) * args.row_bytes + x * VEC) = v;
-    }
-    for (int i = tid; i < moves; i += NT) {
-      const int src = from[i], dst = to[i], ps = table[src / kPageTokens], pd = table[dst / kPageTokens];
-      if (good(ps) && good(pd)) rec[pd * page_recs + dst % kPageTokens] = rec[ps * page_recs + src % kPageTokens];
+    const int n_moves = min(kMoves, end - at);
+    for (int i = tid; i < n_moves; i += NT) {
+      const int src = pairs[i].x, dst = pairs[i].y, ps = table[src / kPageTokens], pd = table[dst / kPageTokens];
+      const bool ok = good(ps) && good(pd);
+      auto row_off = [&](int page, int slot) {
+        return kv_page_off(geom, page, layer, 0) + (size_t)(c * kPageTokens + slot % kPageTokens) * args.row_bytes;
+      };
+      moves[i] = ok ? Move{row_off(ps, src), row_off(pd, dst)} : Move{0, 0};  // (to itself)
+      if (ok && args.records) rec[pd * page_recs + dst % kPageTokens] = rec[ps * page_recs + src % kPageTokens];
     }
     __syncthreads();
+    if (!args.rows) continue;
+    // keys and values of four rows in flight
+    constexpr int U = 4;
+#pragma unroll 1
+    for (int i = r0; i < n_moves; i += U * per_pass)
+#pragma unroll 1
+      for (int x = x0; x < row_words; x += row_lanes) {
+        word k[U], v[U];
+        Move mv[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          mv[u] = moves[min(i + u * per_pass, n_moves - 1)];
+          const char* p = args.slab + mv[u].src + x * VEC;
+          k[u] = *reinterpret_cast<const word*>(p), v[u] = *reinterpret_cast<const word*>(p + geom.block_bytes);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          char* p = args.slab + mv[u].dst + x * VEC;
+          if (i + u * per_pass < n_moves && mv[u].src != mv[u].dst) *reinterpret_cast<word*>(p) = k[u], *reinterpret_cast<word*>(p + geom.block_bytes) = v[u];
+        }
+      }
   }
 }
 
+// Long sequences need more dynamic LDS than the default limit; asked for once per device.
+constexpr int kMaxDevices = 64;
+bool g_evict_lds[kMaxDevices] = {};
+std::mutex g_evict_lds_mu;
+
+harli_status allow_evict_lds() {
+  int dev = -1;
+  HARLI_HIP(hipGetDevice(&dev));
+  if (dev < 0 || dev >= kMaxDevices) return fail(HARLI_ERR_INVALID, "kv_evict: device ordinal %d outside 0..%d", dev, kMaxDevices - 1);
+  std::lock_guard<std::mutex> lk(g_evict_lds_mu);
+  if (!g_evict_lds[dev]) {
+    const void* kernels[] = {reinterpret_cast<const void*>(&k_evict<512, true, 16>), reinterpret_cast<const void*>(&k_evict<512, true, 8>),
+                             reinterpret_cast<const void*>(&k_evict<1024, true, 16>), reinterpret_cast<const void*>(&k_evict<1024, true, 8>)};
+    for (const void* k : kernels) HARLI_HIP(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)evict_lds(kKeysInLds, true)));
+    g_evict_lds[dev] = true;
+  }
+  return HARLI_OK;
+}
+
 template <int VEC>
-void launch_evict(const EvictArgs& a, int heads, int layers, hipStream_t st) {
-  const dim3 grid(heads, a.b.batch, layers);
-  const size_t bits = (size_t)(a.b.max_kv_len + 63) / 64 * 8;
-  if (a.b.max_kv_len <= 256 * 32) hipLaunchKernelGGL((k_evict<256, 32, VEC>), grid, dim3(256), bits, st, a);
-  else if (a.b.max_kv_len <= 1024 * 32) hipLaunchKernelGGL((k_evict<1024, 32, VEC>), grid, dim3(1024), bits, st, a);
-  else hipLaunchKernelGGL((k_evict<1024, 0, VEC>), grid, dim3(1024), bits, st, a);
+harli_status launch_evict(EvictArgs a, int heads, int layers, int n_cu, hipStream_t st) {
+  const int n = a.b.max_kv_len, words = a.row_bytes / VEC;
+  for (a.row_lanes = 1; a.row_lanes < words && a.row_lanes < 64;) a.row_lanes *= 2;
+  const bool keys = n <= kKeysInLds;
+  const size_t lds = evict_lds(n, keys);
+  if (lds > (48u << 10)) {  // (with the kernel's own)
+    const harli_status rc = allow_evict_lds();
+    if (rc != HARLI_OK) return rc;
+  }
+  auto go = [&](bool rows, bool records) {
+    a.rows = rows, a.records = records;
+    if (!rows) a.parts = 1;
+    const dim3 grid(heads * a.parts, a.b.batch, layers);
+    if (n <= 2048) hipLaunchKernelGGL((k_evict<256, true, VEC>), grid, dim3(256), lds, st, a);
+    else if (n <= 16384) hipLaunchKernelGGL((k_evict<512, true, VEC>), grid, dim3(512), lds, st, a);
+    else if (keys) hipLaunchKernelGGL((k_evict<1024, true, VEC>), grid, dim3(1024), lds, st, a);
+    else hipLaunchKernelGGL((k_evict<1024, false, VEC>), grid, dim3(1024), lds, st, a);
+  };
+  // Few long sequences: several workgroups find the same moves and share the rows.  The records they go by must not change
+  // meanwhile, so those move in a launch of their own.
+  const long long heads_all = (long long)heads * layers * a.b.batch;
+  a.parts = n > 2048 ? (int)std::max(1ll, std::min(8ll, n_cu / heads_all)) : 1;
+  if (a.parts == 1) {
+    go(true, true);
+  } else {
+    go(true, false);
+    go(false, true);
+  }
+  return HARLI_OK;
 }
 
 }  // namespace
@@ -245,11 +303,12 @@ extern "C" harli_status harli_kv_evict(harli_ctx* c, const harli_evict_batch* b,
     return fail(HARLI_ERR_INVALID, "kv_evict: n_left is an input");
   if (b->max_kv_len > kMostTokens) return fail(HARLI_ERR_INVALID, "kv_evict: max_kv_len %d above %d", b->max_kv_len, kMostTokens);
   const int row_bytes = (int)(m.head_dim * esize(c));
-  const EvictArgs a{*b, m.n_kv_heads, row_bytes, c->slab, c->geom, c->dw.err_flag};
+  EvictArgs a{};
+  a.b = *b, a.n_kv = m.n_kv_heads, a.row_bytes = row_bytes, a.slab = c->slab, a.geom = c->geom, a.err_flag = c->dw.err_flag;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   // pages start at multiples of 16 rows: rows of whole 16 bytes keep their words aligned, others (fp32, even head sizes) have 8
-  if (row_bytes % 16 == 0) launch_evict<16>(a, m.n_kv_heads, m.n_layers, st);
-  else launch_evict<8>(a, m.n_kv_heads, m.n_layers, st);
+  const harli_status rc = row_bytes % 16 == 0 ? launch_evict<16>(a, m.n_kv_heads, m.n_layers, c->n_cu, st) : launch_evict<8>(a, m.n_kv_heads, m.n_layers, c->n_cu, st);
+  if (rc != HARLI_OK) return rc;
   HARLI_HIP(hipGetLastError());
   return HARLI_OK;
 }
