@@ -15,7 +15,6 @@ namespace {
 
 constexpr int kPageTokens = 16;
 constexpr int kMostPages = 1 << 26;  // of a table row: token indexes stay in 32 bits
-constexpr int kMoves = 512;           // moves listed in LDS at a time
 constexpr int kMostTokens = 1 << 18;  // of a sequence: a bit each in LDS
 constexpr int kBins = 2048;           // of the search for the last weight that stays: 11, 11 and 10 bits
 constexpr int kKeysInLds = 32768;     // tokens whose keys are read once and stay in LDS; of longer sequences they are read again for every pass
@@ -54,11 +53,13 @@ struct EvictArgs {
 
 // LDS: a bit per token that stays, then keys and bins of the search, whose place the moves' offsets take afterwards.
 struct Move {
-  unsigned long long src, dst;  // of a key's row, from the slab's start
+  u64 src, dst;  // of a key's row, from the slab's start
 };
-size_t evict_lds(int max_kv_len, bool keys) {
-  const size_t bits = ((size_t)max_kv_len + 63) / 64 * 8, search = (keys ? ((size_t)max_kv_len + 3) / 4 * 16 : 0) + kBins * 4;
-  return bits + std::max(search, (size_t)kMoves * (sizeof(Move) + 8)) + 16;
+__host__ __device__ constexpr int moves_listed(int threads) { return 2 * threads; }  // at a time
+__host__ __device__ inline size_t bitmap_bytes(int max_kv_len) { return ((size_t)max_kv_len + 127) / 128 * 2 * (8 + 8); }  // and two sums per word
+size_t evict_lds(int max_kv_len, bool keys, int threads) {
+  const size_t search = (keys ? ((size_t)max_kv_len + 3) / 4 * 16 : 0) + kBins * 4;
+  return bitmap_bytes(max_kv_len) + std::max(search, (size_t)moves_listed(threads) * (sizeof(Move) + 8));
 }
 
 // NT threads; KEYS: the keys stay in LDS; rows move in words of VEC bytes.
@@ -66,7 +67,7 @@ size_t evict_lds(int max_kv_len, bool keys) {
 // rounds over keys in registers (39 KB of code: 21.6 us for 16 sequences that give up one page of 1040 tokens in eight layers).
 template <int NT, bool KEYS, int VEC>
 __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
-  constexpr int NW = NT / 64, BPT = kBins / NT;
+  constexpr int NW = NT / 64, BPT = kBins / NT, kMoves = moves_listed(NT);
   static_assert(kBins % NT == 0 && NW <= 16, "whole bins per thread; the waves' sums in a row of lanes");
   const harli_evict_batch& a = args.b;
   const KvGeom& geom = args.geom;
@@ -91,24 +92,35 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
   auto good = [&](int page) { return page >= 0 && page < geom.n_pages_total; };
 
   extern __shared__ __align__(16) char evict_lds_mem[];
-  u64* stays = reinterpret_cast<u64*>(evict_lds_mem);  // a bit per token
-  char* rest = evict_lds_mem + (((size_t)a.max_kv_len + 63) / 64 * 8 + 15) / 16 * 16;
+  const int most_words = (a.max_kv_len + 127) / 128 * 2;
+  u64* stays = reinterpret_cast<u64*>(evict_lds_mem);           // a bit per token
+  int2* sums = reinterpret_cast<int2*>(stays + most_words);     // free slots and moving tokens before each word
+  char* rest = evict_lds_mem + bitmap_bytes(a.max_kv_len);
   int* hist = reinterpret_cast<int*>(rest);
   unsigned* keys = reinterpret_cast<unsigned*>(rest + kBins * 4);
   Move* moves = reinterpret_cast<Move*>(rest);  // once the search is done
   int2* pairs = reinterpret_cast<int2*>(rest + kMoves * sizeof(Move));
   __shared__ int tmp[NW], s_bin, s_above, s_count;
 
+  bool bad = false;
   auto load_key = [&](int t) -> unsigned {  // of a token of the sequence
     const int page = table[t / kPageTokens];
     const bool ok = good(page);
-    if (!ok && first) atomicOr(args.err_flag, 1);
+    bad |= !ok;
     const uint2 r = *reinterpret_cast<const uint2*>(rec + (ok ? page : 0) * page_recs + t % kPageTokens);
     return ok ? rank_key(r, a.sink, recent_from) : 0;
   };
   if constexpr (KEYS) {
-#pragma unroll 4
-    for (int t = tid; t < n; t += NT) keys[t] = load_key(t);
+    constexpr int U = 8;  // tokens of a thread in flight
+#pragma unroll 1
+    for (int t0 = tid; t0 < n; t0 += U * NT) {
+      unsigned k[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) k[u] = load_key(min(t0 + u * NT, n - 1));
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (t0 + u * NT < n) keys[t0 + u * NT] = k[u];
+    }
   }
   auto key_of = [&](int t) { return KEYS ? keys[t] : load_key(t); };
 
@@ -145,6 +157,7 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
     prefix |= (unsigned)s_bin << shift;
     mask |= digits << shift;
   }
+  if (bad && first) atomicOr(args.err_flag, 1);
   __syncthreads();
 
   // ---- who stays: 64 tokens in a row are a ballot ---------------------------------------------------------------------------
@@ -178,23 +191,30 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
   auto movers_of = [&](int w) { return stays[w] & ~below(keep - 64 * w); };
   int holes = 0, movers = 0, total, total_movers;
   for (int w = w_lo; w < w_hi; ++w) holes += __popcll(holes_of(w)), movers += __popcll(movers_of(w));
-  const int h0 = scan_before<NW>(holes, tmp, lane, wave, total), m0 = scan_before<NW>(movers, tmp, lane, wave, total_movers);
+  holes = scan_before<NW>(holes, tmp, lane, wave, total), movers = scan_before<NW>(movers, tmp, lane, wave, total_movers);
+  for (int w = w_lo; w < w_hi; ++w) {
+    sums[w] = make_int2(holes, movers);
+    holes += __popcll(holes_of(w)), movers += __popcll(movers_of(w));
+  }
   typedef unsigned int __attribute__((ext_vector_type(VEC / 4))) word;
   const int row_words = args.row_bytes / VEC, row_lanes = args.row_lanes, per_pass = NT / row_lanes, x0 = tid & (row_lanes - 1), r0 = tid / row_lanes;
   const int share = (total + args.parts - 1) / args.parts, end = min(total, (part + 1) * share);
 #pragma unroll 1
   for (int at = part * share; at < end; at += kMoves) {
     __syncthreads();
-    int h = h0 - at, m = m0 - at;
-    for (int w = w_lo; w < w_hi; ++w) {
-      const u64 hs = holes_of(w), ms = movers_of(w);
-      if (h < kMoves && h + (int)__popcll(hs) > 0)
-        for (u64 x = hs, i = h; x; x &= x - 1, ++i)
-          if ((int)i >= 0 && (int)i < kMoves) pairs[i].y = 64 * w + __ffsll(x) - 1;
-      if (m < kMoves && m + (int)__popcll(ms) > 0)
-        for (u64 x = ms, i = m; x; x &= x - 1, ++i)
-          if ((int)i >= 0 && (int)i < kMoves) pairs[i].x = 64 * w + __ffsll(x) - 1;
-      h += __popcll(hs), m += __popcll(ms);
+#pragma unroll 2
+    for (int t = tid; t < n; t += NT) {  // (a wave: one word)
+      const int w = t / 64;
+      const u64 lower = (1ull << lane) - 1;
+      const int2 before = sums[w];
+      const bool in = stays[w] >> lane & 1;
+      if (t < keep) {
+        const int i = before.x + (int)__popcll(~stays[w] & lower) - at;
+        if (!in && i >= 0 && i < kMoves) pairs[i].y = t;
+      } else {
+        const int i = before.y + (int)__popcll(movers_of(w) & lower) - at;
+        if (in && i >= 0 && i < kMoves) pairs[i].x = t;
+      }
     }
     __syncthreads();
     const int n_moves = min(kMoves, end - at);
@@ -244,8 +264,10 @@ harli_status allow_evict_lds() {
   std::lock_guard<std::mutex> lk(g_evict_lds_mu);
   if (!g_evict_lds[dev]) {
     const void* kernels[] = {reinterpret_cast<const void*>(&k_evict<512, true, 16>), reinterpret_cast<const void*>(&k_evict<512, true, 8>),
-                             reinterpret_cast<const void*>(&k_evict<1024, true, 16>), reinterpret_cast<const void*>(&k_evict<1024, true, 8>)};
-    for (const void* k : kernels) HARLI_HIP(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)evict_lds(kKeysInLds, true)));
+                             reinterpret_cast<const void*>(&k_evict<1024, true, 16>), reinterpret_cast<const void*>(&k_evict<1024, true, 8>),
+                             reinterpret_cast<const void*>(&k_evict<1024, false, 16>), reinterpret_cast<const void*>(&k_evict<1024, false, 8>)};
+    const size_t most = std::max(evict_lds(kKeysInLds, true, 1024), evict_lds(kMostTokens, false, 1024));
+    for (const void* k : kernels) HARLI_HIP(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)most));
     g_evict_lds[dev] = true;
   }
   return HARLI_OK;
@@ -256,7 +278,8 @@ harli_status launch_evict(EvictArgs a, int heads, int layers, int n_cu, hipStrea
   const int n = a.b.max_kv_len, words = a.row_bytes / VEC;
   for (a.row_lanes = 1; a.row_lanes < words && a.row_lanes < 64;) a.row_lanes *= 2;
   const bool keys = n <= kKeysInLds;
-  const size_t lds = evict_lds(n, keys);
+  const int threads = n <= 2048 ? 256 : n <= 16384 ? 512 : 1024;
+  const size_t lds = evict_lds(n, keys, threads);
   if (lds > (48u << 10)) {  // (with the kernel's own)
     const harli_status rc = allow_evict_lds();
     if (rc != HARLI_OK) return rc;
@@ -265,8 +288,8 @@ harli_status launch_evict(EvictArgs a, int heads, int layers, int n_cu, hipStrea
     a.rows = rows, a.records = records;
     if (!rows) a.parts = 1;
     const dim3 grid(heads * a.parts, a.b.batch, layers);
-    if (n <= 2048) hipLaunchKernelGGL((k_evict<256, true, VEC>), grid, dim3(256), lds, st, a);
-    else if (n <= 16384) hipLaunchKernelGGL((k_evict<512, true, VEC>), grid, dim3(512), lds, st, a);
+    if (threads == 256) hipLaunchKernelGGL((k_evict<256, true, VEC>), grid, dim3(256), lds, st, a);
+    else if (threads == 512) hipLaunchKernelGGL((k_evict<512, true, VEC>), grid, dim3(512), lds, st, a);
     else if (keys) hipLaunchKernelGGL((k_evict<1024, true, VEC>), grid, dim3(1024), lds, st, a);
     else hipLaunchKernelGGL((k_evict<1024, false, VEC>), grid, dim3(1024), lds, st, a);
   };
