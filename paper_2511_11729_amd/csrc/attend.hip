@@ -4,11 +4,13 @@
 // only now that the maximum and the sum over all chunks are known:  P_j = exp2(s_j - M) / L.
 // What bounds it: HBM, for keys and values (2 d e bytes per token and KV head).  The scores are 4 bytes per token and query head,
 // written once and read back from the caches, and the records 8 + 8 bytes per token and KV head.
+#include <algorithm>
 #include <cmath>
 
 #include "attend.h"
 #include "decode_large.h"
 #include "device_utils.h"
+#include "scan_utils.h"
 
 namespace harli {
 namespace {
@@ -16,7 +18,8 @@ namespace {
 constexpr int kPageTokens = 16;
 constexpr int kMostPages = 1 << 26;  // of a table row: token indexes stay in 32 bits
 constexpr int kChunkF32 = 256;    // tokens per chunk on fp32 storage: one per thread
-constexpr int kFinishTokens = 1024;  // tokens per workgroup of the records: four per thread
+constexpr int kFinishTokens = 1024;  // tokens of a block of records: four per thread
+constexpr int kPiece = 64;           // elements of an output row that are joined at a time
 
 // fp32 storage: one chunk of one query head; a thread scores one token, then a wave adds up P.V of every fourth token with a lane
 // per element.  EL: elements per lane; a head larger than 64 EL goes to several workgroups (blockIdx.z), which score it alike.
@@ -97,120 +100,130 @@ __global__ void __launch_bounds__(256) k_attend_f32(const float* q, const int* k
 
 struct FinishArgs {
   const int *kv_len, *page_table, *position;
-  int max_pages, layer, n_q, n_kv, d, n_pages;
+  int max_pages, layer, n_q, n_kv, d, n_pages, parts;
   float* out;
   unsigned short* frag;
   harli_kv_record* records;
   float decay;
 };
 
-// maximum and reciprocal sum over the chunks of one head, the same in every lane (wave collective)
-__device__ __forceinline__ void joined(const float* ml, int nch, int lane, float& M, float& inv) {
-  float m = -INFINITY, l = 0.f;
-  for (int i = lane; i < nch; i += 64) {
-    const float2 v = *reinterpret_cast<const float2*>(ml + 2 * i);
-    const float mn = fmaxf(m, v.x);
-    if (mn > -INFINITY) l = l * exp2f(m - mn) + v.y * exp2f(v.x - mn);
-    m = mn;
-  }
-  float all = m;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) all = fmaxf(all, __shfl_xor(all, o, 64));
-  M = all == -INFINITY ? 0.f : all;
-  l = wave_sum(l * exp2f(m - M));
-  inv = l == 0.f ? 0.f : 1.f / l;  // no token that counts: zeros
-}
-
-// Workgroups [0, n_q): the output row of a query head, VEC elements a lane and as many chunks side by side as lanes are left.
-// The others: the records of kFinishTokens tokens of a KV head.
+// A KV head of a sequence is `parts` workgroups.  Each finds the maximum and the sum of every query head over the chunks, and then takes its
+// share of the blocks of records and of the pieces of output rows: VEC elements a lane, kPiece / VEC lanes a piece, chunks side by side.
+// What it costs is the latency of its steps, so the first block's scores and records are on their way before the sums are needed.
 template <int VEC>
 __global__ void __launch_bounds__(256) k_attend_finish(FinishArgs a, AttendWs att) {
+  extern __shared__ float s_ml[];  // [heads of the group][maximum, 1 / sum]
+  __shared__ float red[256 * VEC];
+  constexpr int HP = 8;  // query heads whose scores are fetched ahead
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int part = blockIdx.x / a.n_kv, c = blockIdx.x - part * a.n_kv, G = a.n_q / a.n_kv;
   const int n = max(0, min(min(a.kv_len[b] + att.n_new, att.n_chunks * att.chunk), a.max_pages * kPageTokens));
   const int nch = (n + att.chunk - 1) / att.chunk;
-  __shared__ float red[256 * VEC];
-  if ((int)blockIdx.x < a.n_q) {
-    const int h = blockIdx.x, dv = a.d / VEC, nl = min(dv, 256), ng = 256 / nl, gi = tid / nl;
-    const size_t at = ((size_t)b * a.n_q + h) * att.n_chunks;
-    float M, inv;
-    joined(att.ml + at * 2, nch, lane, M, inv);
-    for (int e0 = 0; e0 < dv; e0 += nl) {
-      const int e = e0 + tid - gi * nl;
-      float acc[VEC];
+  const size_t head0 = (size_t)b * a.n_q + c * G;
+  const float* ml = att.ml + head0 * att.n_chunks * 2;
+  int t = part * kFinishTokens + tid * 4;
+  const bool record = att.scores != nullptr;
+
+  float4 sc[HP];
+  int page = -1;
+  uint4 r[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+  auto fetch = [&](int tokens_at) {
+    t = tokens_at;
+    if (!record || t >= n) return;
+    page = a.page_table[(size_t)b * a.max_pages + t / kPageTokens];
 #pragma unroll
-      for (int x = 0; x < VEC; ++x) acc[x] = 0.f;
-      if (gi < ng && e < dv) {
-#pragma unroll 4
-        for (int i = gi; i < nch; i += ng) {
-          const float f = exp2f(att.ml[(at + i) * 2] - M);
-          float v[VEC];
-          __builtin_memcpy(v, att.o + (at + i) * a.d + e * VEC, VEC * 4);
-#pragma unroll
-          for (int x = 0; x < VEC; ++x) acc[x] += v[x] * f;
-        }
-      }
-#pragma unroll
-      for (int x = 0; x < VEC; ++x) red[tid * VEC + x] = acc[x];
-      __syncthreads();
-      if (tid < nl && e < dv) {
-        for (int g = 1; g < ng; ++g)
-#pragma unroll
-          for (int x = 0; x < VEC; ++x) acc[x] += red[(g * nl + tid) * VEC + x];
-#pragma unroll
-        for (int x = 0; x < VEC; ++x) {
-          const float v = acc[x] * inv;
-          const int k = h * a.d + e * VEC + x;
-          if (a.frag) a.frag[xfrag_off(b, k, (a.n_q * a.d + 31) >> 5)] = f2bf(v);
-          else a.out[(size_t)b * a.n_q * a.d + k] = v;
-        }
-      }
-      __syncthreads();
-    }
-    return;
+    for (int h = 0; h < HP; ++h)
+      if (h < G) sc[h] = *reinterpret_cast<const float4*>(att.scores + (head0 + h) * att.score_ld + t);
+  };
+  auto record_at = [&] { return a.records + (((size_t)a.layer * a.n_pages + page) * a.n_kv + c) * kPageTokens + t % kPageTokens; };
+  fetch(t);
+
+  // ---- maximum and sum of every query head, a wave each
+  for (int h = wave; h < G; h += 4) {
+    const float2* p = reinterpret_cast<const float2*>(ml + (size_t)h * att.n_chunks * 2);
+    const float2 mine = lane < nch ? p[lane] : make_float2(-INFINITY, 0.f);
+    float m = mine.x;
+    for (int i = lane + 64; i < nch; i += 64) m = fmaxf(m, p[i].x);
+    m = wave_top(m);
+    m = m == -INFINITY ? 0.f : m;
+    float l = mine.y * exp2f(mine.x - m);
+    for (int i = lane + 64; i < nch; i += 64) l += p[i].y * exp2f(p[i].x - m);
+    l = lane_value(wave_scan(l), 63);
+    if (lane == 0) s_ml[2 * h] = m, s_ml[2 * h + 1] = l == 0.f ? 0.f : 1.f / l;  // no token that counts: zeros
   }
-  const int blk = (blockIdx.x - a.n_q) / a.n_kv, c = blockIdx.x - a.n_q - blk * a.n_kv, G = a.n_q / a.n_kv;
-  if (blk * kFinishTokens >= n) return;
-  const int t = blk * kFinishTokens + tid * 4;
-  float* s_m = red;
-  float* s_inv = red + 8;
-  float got[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int h0 = 0; h0 < G; h0 += 8) {  // eight query heads at a time
-    __syncthreads();
-    for (int h = wave; h < min(8, G - h0); h += 4) {
-      float M, inv;
-      joined(att.ml + ((size_t)b * a.n_q + c * G + h0 + h) * att.n_chunks * 2, nch, lane, M, inv);
-      if (lane == 0) s_m[h] = M, s_inv[h] = inv;
-    }
-    __syncthreads();
-    if (t < n) {
-#pragma unroll 4
-      for (int h = 0; h < min(8, G - h0); ++h) {
-        const float4 s = *reinterpret_cast<const float4*>(att.scores + ((size_t)b * a.n_q + c * G + h0 + h) * att.score_ld + t);
-        const float M = s_m[h], inv = s_inv[h];
+  __syncthreads();
+
+  // ---- records
+#pragma unroll 1
+  for (; record && t - tid * 4 < n;) {
+    if (t < n && page >= 0 && page < a.n_pages) {  // (another page id is reported where its keys were asked for)
+      harli_kv_record* rec = record_at();
+      r[0] = reinterpret_cast<const uint4*>(rec)[0], r[1] = reinterpret_cast<const uint4*>(rec)[1];
+      float got[4] = {0.f, 0.f, 0.f, 0.f};
+      auto add = [&](int h, const float4& s) {
+        const float M = s_ml[2 * h], inv = s_ml[2 * h + 1];
         got[0] += __builtin_amdgcn_exp2f(s.x - M) * inv;
         got[1] += __builtin_amdgcn_exp2f(s.y - M) * inv;
         got[2] += __builtin_amdgcn_exp2f(s.z - M) * inv;
         got[3] += __builtin_amdgcn_exp2f(s.w - M) * inv;
+      };
+#pragma unroll
+      for (int h = 0; h < HP; ++h)
+        if (h < G) add(h, sc[h]);
+      for (int h = HP; h < G; ++h) add(h, *reinterpret_cast<const float4*>(att.scores + (head0 + h) * att.score_ld + t));
+      unsigned* w[4] = {&r[0].x, &r[0].z, &r[1].x, &r[1].z};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool newest = t + i == n - 1;
+        const float old = newest || a.decay == 0.f ? 0.f : a.decay * __uint_as_float(*w[i]);
+        *w[i] = __float_as_uint(old + got[i]);
+        if (newest) w[i][1] = (unsigned)(a.position ? a.position[b] : n - 1);
+      }
+      if (t + 4 <= n) {
+        reinterpret_cast<uint4*>(rec)[0] = r[0], reinterpret_cast<uint4*>(rec)[1] = r[1];
+      } else {
+        for (int i = 0; i < n - t; ++i) reinterpret_cast<uint2*>(rec)[i] = make_uint2(w[i][0], w[i][1]);
       }
     }
+    fetch(t + a.parts * kFinishTokens);
   }
-  if (t >= n) return;
-  const int page = a.page_table[(size_t)b * a.max_pages + t / kPageTokens];
-  if (page < 0 || page >= a.n_pages) return;  // reported where its keys were asked for
-  harli_kv_record* rec = a.records + (((size_t)a.layer * a.n_pages + page) * a.n_kv + c) * kPageTokens + t % kPageTokens;
-  uint4 r[2] = {reinterpret_cast<const uint4*>(rec)[0], reinterpret_cast<const uint4*>(rec)[1]};
-  unsigned* w[4] = {&r[0].x, &r[0].z, &r[1].x, &r[1].z};
+
+  // ---- output rows
+  constexpr int NL = kPiece / VEC, NG = 256 / NL;
+  const int per_row = (a.d + kPiece - 1) / kPiece, gi = tid / NL;
+#pragma unroll 1
+  for (int piece = part; piece < G * per_row; piece += a.parts) {
+    const int h = piece / per_row, e = (piece - h * per_row) * kPiece + (tid - gi * NL) * VEC;
+    const size_t at = (head0 + h) * att.n_chunks;
+    const float M = s_ml[2 * h];
+    float acc[VEC];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const bool newest = t + i == n - 1;
-    const float old = newest || a.decay == 0.f ? 0.f : a.decay * __uint_as_float(*w[i]);
-    *w[i] = __float_as_uint(old + got[i]);
-    if (newest) w[i][1] = (unsigned)(a.position ? a.position[b] : n - 1);
-  }
-  if (t + 4 <= n) {
-    reinterpret_cast<uint4*>(rec)[0] = r[0], reinterpret_cast<uint4*>(rec)[1] = r[1];
-  } else {
-    for (int i = 0; i < n - t; ++i) reinterpret_cast<uint2*>(rec)[i] = make_uint2(w[i][0], w[i][1]);
+    for (int x = 0; x < VEC; ++x) acc[x] = 0.f;
+    if (e < a.d) {
+#pragma unroll 8
+      for (int i = gi; i < nch; i += NG) {
+        const float f = exp2f(att.ml[(at + i) * 2] - M);
+        float v[VEC];
+        __builtin_memcpy(v, __builtin_assume_aligned(att.o + (at + i) * a.d + e, VEC * 4), VEC * 4);
+#pragma unroll
+        for (int x = 0; x < VEC; ++x) acc[x] += v[x] * f;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < VEC; ++x) red[(gi * NL + (tid - gi * NL)) * VEC + x] = acc[x];
+    __syncthreads();
+    for (int x = tid; x < kPiece; x += 256) {
+      const int k = (piece - h * per_row) * kPiece + x;
+      if (k >= a.d) continue;
+      float v = 0.f;
+#pragma unroll
+      for (int g = 0; g < NG; ++g) v += red[g * kPiece + x];
+      v *= s_ml[2 * h + 1];
+      const int col = (c * G + h) * a.d + k;
+      if (a.frag) a.frag[xfrag_off(b, col, (a.n_q * a.d + 31) >> 5)] = f2bf(v);
+      else a.out[(size_t)b * a.n_q * a.d + col] = v;
+    }
   }
 }
 
@@ -275,12 +288,16 @@ void attend_f32(harli_ctx* c, const float* q, const int* kv_len, const int* page
 void attend_finish(harli_ctx* c, const AttendWs& att, const int* kv_len, const int* page_table, int batch, int max_pages, int layer,
                    float* out, unsigned short* frag, const harli_tracking* t, hipStream_t st) {
   const harli_model_cfg& m = c->cfg;
-  const FinishArgs a{kv_len, page_table, t->position, max_pages, layer, m.n_q_heads, m.n_kv_heads, m.head_dim, c->geom.n_pages_total,
+  // Enough workgroups for the chip, as far as there is work for them: blocks of records and pieces of rows.
+  const int G = m.n_q_heads / m.n_kv_heads, blocks = att.scores ? (att.score_ld + kFinishTokens - 1) / kFinishTokens : 0;
+  const int most = std::max(blocks, G * ((m.head_dim + kPiece - 1) / kPiece));
+  const int parts = std::max(1, std::min(most, 16 * c->n_cu / (batch * m.n_kv_heads)));
+  const FinishArgs a{kv_len, page_table, t->position, max_pages, layer, m.n_q_heads, m.n_kv_heads, m.head_dim, c->geom.n_pages_total, parts,
                      out, frag, t->records, t->decay};
-  const int blocks = att.scores ? (att.score_ld + kFinishTokens - 1) / kFinishTokens * m.n_kv_heads : 0;
-  const dim3 grid(m.n_q_heads + blocks, batch);
-  if (m.head_dim % 4 == 0) hipLaunchKernelGGL(k_attend_finish<4>, grid, dim3(256), 0, st, a, att);
-  else hipLaunchKernelGGL(k_attend_finish<2>, grid, dim3(256), 0, st, a, att);
+  const dim3 grid(m.n_kv_heads * parts, batch);
+  const size_t lds = (size_t)G * 8;
+  if (m.head_dim % 4 == 0) hipLaunchKernelGGL(k_attend_finish<4>, grid, dim3(256), lds, st, a, att);
+  else hipLaunchKernelGGL(k_attend_finish<2>, grid, dim3(256), lds, st, a, att);
 }
 
 }  // namespace harli

@@ -1166,14 +1166,15 @@ namespace harli {
 
 int attend_chunk_bf16(int d, int G) { return attn_chunk(d, G); }
 
-// The chunks of harli_kv_attend on bf16 storage (k_attend_finish joins them).
+// The chunks of harli_kv_attend on bf16 storage (k_attend_finish joins them).  Keys and values are nontemporal loads at every size: a
+// program reads the other layers' caches, and the weights, before it comes back to these (16 sequences of 8 KV heads, 16 to 131 MB,
+// ordinary / nontemporal: three caches in turn 19.2 / 19.3 to 55.2 / 50.0 us, one again and again 17.3 / 17.5 to 47.0 / 50.1).
 harli_status attend_bf16(harli_ctx* c, const harli_attend_batch* b, const AttendWs& att, hipStream_t st) {
   AttnList list{};
   list.chunk = att.chunk;
   list.n_chunks = att.n_chunks;
-  const size_t kv = (size_t)b->batch * b->max_kv_len * c->cfg.n_kv_heads * c->cfg.head_dim * 4;  // keys and values, two bytes each
   const AttnArgs a{b->q, b->n_tokens, b->page_table, b->batch, b->max_pages, b->layer, nullptr, 0, nullptr};
-  return dispatch_attn<true>(c, a, kv <= kMemorySideCache, list, att, st);
+  return dispatch_attn<true>(c, a, false, list, att, st);
 }
 
 harli_status decode_step_f32(harli_ctx* c, const harli_decode_batch* b, hipStream_t st, const harli_tracking* tr);  // decode_generic.hip

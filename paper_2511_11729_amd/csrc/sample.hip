@@ -12,7 +12,6 @@
 // What bounds it: HBM for the logits in the first launch, with the exponential in 64 bits close behind it (20 instructions per token: 20 us for
 // 256 rows of 152064 against 26 us of reading); in the second the latency of its steps.
 #include <mutex>
-#include <type_traits>
 
 #include "ctx.h"
 #include "device_utils.h"
@@ -128,17 +127,6 @@ struct SampleWs {
   unsigned short* upto_count;  // [kLogitBins] tokens of them
   int n;             // stretches per row
 };
-
-__device__ __forceinline__ float wave_top(float v) {  // of values that are not NaN
-  auto step = [&](auto ctrl) { v = fmaxf(v, __uint_as_float((unsigned)__builtin_amdgcn_update_dpp((int)0xff800000, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, false))); };
-  step(std::integral_constant<int, 0x111>{});
-  step(std::integral_constant<int, 0x112>{});
-  step(std::integral_constant<int, 0x114>{});
-  step(std::integral_constant<int, 0x118>{});
-  step(std::integral_constant<int, 0x142>{});
-  step(std::integral_constant<int, 0x143>{});
-  return lane_value(v, 63);
-}
 
 constexpr int kStretchThreads = 256, kPer = kStretch / kStretchThreads;
 

@@ -2,6 +2,8 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 namespace harli {
 
 typedef unsigned long long u64;
@@ -42,6 +44,17 @@ __device__ __forceinline__ T lane_value(T v, int lane) {  // lane: uniform
   } else {
     return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
   }
+}
+
+__device__ __forceinline__ float wave_top(float v) {  // of values that are not NaN
+  auto step = [&](auto ctrl) { v = fmaxf(v, __uint_as_float((unsigned)__builtin_amdgcn_update_dpp((int)0xff800000, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, false))); };
+  step(std::integral_constant<int, 0x111>{});
+  step(std::integral_constant<int, 0x112>{});
+  step(std::integral_constant<int, 0x114>{});
+  step(std::integral_constant<int, 0x118>{});
+  step(std::integral_constant<int, 0x142>{});
+  step(std::integral_constant<int, 0x143>{});
+  return lane_value(v, 63);
 }
 
 }  // namespace harli
