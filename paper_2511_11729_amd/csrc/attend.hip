@@ -20,6 +20,7 @@ constexpr int kMostPages = 1 << 26;  // of a table row: token indexes stay in 32
 constexpr int kChunkF32 = 256;    // tokens per chunk on fp32 storage: one per thread
 constexpr int kFinishTokens = 1024;  // tokens of a block of records: four per thread
 constexpr int kPiece = 64;           // elements of an output row that are joined at a time
+constexpr int kFewChunks = 16;       // up to here an output element is one thread's
 
 // fp32 storage: one chunk of one query head; a thread scores one token, then a wave adds up P.V of every fourth token with a lane
 // per element.  EL: elements per lane; a head larger than 64 EL goes to several workgroups (blockIdx.z), which score it alike.
@@ -188,7 +189,25 @@ __global__ void __launch_bounds__(256) k_attend_finish(FinishArgs a, AttendWs at
     fetch(t + a.parts * kFinishTokens);
   }
 
-  // ---- output rows
+  auto store = [&](int col, float v) {  // element col of the sequence's row
+    if (a.frag) a.frag[xfrag_off(b, col, (a.n_q * a.d + 31) >> 5)] = f2bf(v);
+    else a.out[(size_t)b * a.n_q * a.d + col] = v;
+  };
+  // ---- output rows of few chunks: an element per thread
+  if (nch <= kFewChunks) {
+#pragma unroll 1
+    for (int i = part * 256 + tid; i < G * a.d; i += a.parts * 256) {
+      const int h = i / a.d, e = i - h * a.d;
+      const size_t at = (head0 + h) * att.n_chunks;
+      const float M = s_ml[2 * h];
+      float v = 0.f;
+#pragma unroll 8
+      for (int j = 0; j < nch; ++j) v += att.o[(at + j) * a.d + e] * exp2f(att.ml[(at + j) * 2] - M);
+      store(c * G * a.d + i, v * s_ml[2 * h + 1]);
+    }
+    return;
+  }
+  // ---- of many
   constexpr int NL = kPiece / VEC, NG = 256 / NL;
   const int per_row = (a.d + kPiece - 1) / kPiece, gi = tid / NL;
 #pragma unroll 1
@@ -220,9 +239,7 @@ __global__ void __launch_bounds__(256) k_attend_finish(FinishArgs a, AttendWs at
 #pragma unroll
       for (int g = 0; g < NG; ++g) v += red[g * kPiece + x];
       v *= s_ml[2 * h + 1];
-      const int col = (c * G + h) * a.d + k;
-      if (a.frag) a.frag[xfrag_off(b, col, (a.n_q * a.d + 31) >> 5)] = f2bf(v);
-      else a.out[(size_t)b * a.n_q * a.d + col] = v;
+      store((c * G + h) * a.d + k, v);
     }
   }
 }
