@@ -52,6 +52,13 @@ __global__ void __launch_bounds__(256) k_attend_f32(const float* q, const int* k
       const float* qe = EL < 16 ? qs : qv;
       s = 0.f;
       int e = 0;
+      for (; e + 64 <= d; e += 64) {  // a whole 256 bytes in flight
+        float kv[64];
+#pragma unroll
+        for (int x = 0; x < 64; x += 4) __builtin_memcpy(kv + x, kp + e + x, 16);
+#pragma unroll
+        for (int x = 0; x < 64; x += 4) s += qe[e + x] * kv[x] + qe[e + x + 1] * kv[x + 1] + qe[e + x + 2] * kv[x + 2] + qe[e + x + 3] * kv[x + 3];
+      }
 #pragma unroll 4
       for (; e + 4 <= d; e += 4) {
         float kv[4];
@@ -81,14 +88,18 @@ __global__ void __launch_bounds__(256) k_attend_f32(const float* q, const int* k
   float acc[EL];
 #pragma unroll
   for (int x = 0; x < EL; ++x) acc[x] = 0.f;
-#pragma unroll 4
-  for (int u = wave; u < nt; u += 4) {
-    const long long a = at[u];
-    const float pu = ps[u];
+  constexpr int U = EL >= 16 ? 1 : 8;  // tokens of a wave in flight
+  for (int u0 = wave; u0 < nt; u0 += 4 * U) {
+    float v[U][EL];
 #pragma unroll
-    for (int x = 0; x < EL; ++x) {
-      const int e = e0 + lane + 64 * x;
-      if (a >= 0 && e < d) acc[x] += pu * base[a + e];
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int x = 0; x < EL; ++x) v[u][x] = base[max(at[min(u0 + 4 * u, nt - 1)], 0ll) + min(e0 + lane + 64 * x, d - 1)];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float pu = u0 + 4 * u < nt && at[min(u0 + 4 * u, nt - 1)] >= 0 ? ps[u0 + 4 * u] : 0.f;
+#pragma unroll
+      for (int x = 0; x < EL; ++x) acc[x] = pu != 0.f ? acc[x] + pu * v[u][x] : acc[x];
     }
   }
 #pragma unroll
