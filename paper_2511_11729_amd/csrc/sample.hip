@@ -246,7 +246,7 @@ constexpr int kListed = kCandidates / kRowWaves;   // tokens of the bin a wave c
 struct RowShared {
   u64 digit[kDigits];
   double powers[kPowersN];
-  unsigned key[kCandidates], index[kCandidates];
+  uint2 listed[kCandidates];      // (logit's bits, index); then (key, index)
   float top[kMostStretches];
   int below[kMostStretches];      // bins from the row's first to the stretch's
   double scale[kMostStretches];   // of the stretch's sums to the row's, which are relative to its largest logit
@@ -425,14 +425,25 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
       const int g = tid & (kLogitBins - 1), grp = tid / kLogitBins;
       double m = 0;
       unsigned c = 0;
-#pragma unroll 5
-      for (int i = grp; i < NS; i += NG) {
-        const int j = g - sh.below[i];
-        const size_t e = (at0 + i) * kLogitBins + max(j, 0);
-        const double x = ws.upto_weight[e];
-        const unsigned n = s.k ? ws.upto_count[e] : 0;
-        m += j >= 0 ? x * sh.scale[i] : 0.0;
-        c += j >= 0 ? n : 0;
+      constexpr int U = 10;  // stretches of a thread in flight
+#pragma unroll 1
+      for (int i0 = grp; i0 < NS; i0 += U * NG) {
+        double x[U];
+        unsigned n[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int i = min(i0 + u * NG, NS - 1);
+          const size_t e = (at0 + i) * kLogitBins + max(g - sh.below[i], 0);
+          x[u] = ws.upto_weight[e];
+          n[u] = s.k ? ws.upto_count[e] : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int i = min(i0 + u * NG, NS - 1);
+          const bool in = i0 + u * NG < NS && g >= sh.below[i];
+          m += in ? x[u] * sh.scale[i] : 0.0;
+          c += in ? n[u] : 0;
+        }
       }
       sh.part[grp][g] = m, sh.part_n[grp][g] = c;
       __syncthreads();
@@ -478,7 +489,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
         if (!t_key) break;
         bin = bin_of(t_key);
       }
-      if (far) bin = kLogitBins;
+      if (far || infinite) bin = kLogitBins;
 
       // ---- the tokens of the bin, in LDS (their order there is of no account)
       if (bin < kLogitBins && bin != held) {
@@ -522,25 +533,24 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
           }
 #pragma unroll
           for (int r = 0; r < R; ++r) {
-            const int x = now + r * 64 + lane;
-            const float f = infinite ? finite_row(v[r]) : v[r];
-            const bool in = f >= border[0] && f < border[1] && x < V;
+            const bool in = v[r] >= border[0] && v[r] < border[1] && lane < V - now - r * 64;
             const u64 who = __ballot(in);
             if (who) {
-              const int at = listed + (int)__popcll(who & ((1ull << lane) - 1));
-              if (in && at < kListed) sh.key[wave * kListed + at] = order_key(f), sh.index[wave * kListed + at] = (unsigned)x;
+              const int at = listed + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(who >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)who, 0u));
+              if (in && at < kListed) sh.listed[wave * kListed + at] = make_uint2(__float_as_uint(v[r]), (unsigned)(now + r * 64 + lane));
               listed += __popcll(who);
             }
           }
         }
         if (listed > kListed && lane == 0) sh.overflow = 1;
+        for (int i = lane; i < min(listed, kListed); i += 64) sh.listed[wave * kListed + i].x = order_key(__uint_as_float(sh.listed[wave * kListed + i].x));
         __syncthreads();
       }
       in_lds = bin < kLogitBins && sh.overflow == 0;
       // what the search looks at: the listed tokens, every wave its own, or all of the row
       const int from = in_lds ? wave * kListed + lane : tid, end = in_lds ? wave * kListed + listed : V, step = in_lds ? 64 : kRowThreads;
       auto key_at = [&](int i) {
-        if (in_lds) return sh.key[i];
+        if (in_lds) return sh.listed[i].x;
         const float v = logit(i);
         return usable(v) ? order_key(v) : 0u;
       };
@@ -555,7 +565,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
         bits = 20;
       } else if (in_lds) {  // the highest bit in which the listed tokens differ
         unsigned ones = 0, zeros = 0;
-        for (int i = from; i < end; i += step) ones |= sh.key[i], zeros |= ~sh.key[i];
+        for (int i = from; i < end; i += step) ones |= sh.listed[i].x, zeros |= ~sh.listed[i].x;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) ones |= (unsigned)__shfl_xor((int)ones, o, 64), zeros |= (unsigned)__shfl_xor((int)zeros, o, 64);
         if (lane == 0) sh.wave_u[wave] = ones, sh.wave_u[kRowWaves + wave] = zeros;
@@ -573,7 +583,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
       }
       const unsigned key = find_key(
           from, end, step, common, bits,
-          [&](int i) { return phase == 2 ? (unsigned)(kMostVocab - 1) - (in_lds ? sh.index[i] : (unsigned)i) : key_at(i); },
+          [&](int i) { return phase == 2 ? (unsigned)(kMostVocab - 1) - (in_lds ? sh.listed[i].y : (unsigned)i) : key_at(i); },
           [&](int i) -> u64 {
             const unsigned k = key_at(i);
             return phase == 2 ? k == t_key : k == 0 ? 0 : phase == 0 ? 1 : row_weight(k) >> wide_sum;
@@ -607,7 +617,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
         for (int i = tid; i < NS; i += kRowThreads) sh.inside[i] = 0;
         __syncthreads();
         for (int i = wave * kListed + lane; i < wave * kListed + listed; i += 64) {
-          const unsigned k = sh.key[i], x = sh.index[i];
+          const unsigned k = sh.listed[i].x, x = sh.listed[i].y;
           if (k > t_key || (k == t_key && x <= last)) atomicAdd(&sh.inside[x / kStretch], row_weight(k));
         }
         __syncthreads();
