@@ -176,18 +176,19 @@ __global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample
   const bool far = !(fabs(ceiling) < kFarStretch);
   u64 sum = 0;
   unsigned count = 0;
-  // Logits below the bins and below all weights (2^-60) are taken as the one at that border.  This is the loop that the launch's time
+  // Logits below the bins and below all weights (2^-60) are taken as the one at that border, or the next below it that is a float.  This is the loop that the launch's time
   // goes into: conversions between 64-bit floating point and integers, and ldexp, are slow beside sums and products, hence the sums beside
   // kWholes and the exponent added as bits.
-  const double border = (ceiling - (double)(max(60 * 64, kLogitBins << shift) + 64)) / per_t;
-  const float least = border > -3e38 ? (float)border : -INFINITY;
+  const int deepest = max(60 * 64, kLogitBins << shift) + 64;  // wholes; 2^-513 at most
+  const double border = (ceiling - (double)deepest) / per_t;
+  const float nearest = (float)border, least = border > -3e38 ? ((double)nearest <= border ? nearest : nextafterf(nearest, -INFINITY)) : -INFINITY;
   const double wholes = kWholes + ceiling;
   double c3 = series.c3;
   asm("" : "+v"(c3));  // (one scalar operand per instruction)
   auto add = [&](float x, bool masked) {
     x = __builtin_amdgcn_fmed3f(x, least, INFINITY);  // (least for NaN too)
     const double d = (double)x, y = fma(d, -per_t, wholes), f = fma(d, per_t, y - wholes);
-    const unsigned below = (unsigned)(u64)__double_as_longlong(y);  // wholes below the ceiling
+    const unsigned below = min((unsigned)(u64)__double_as_longlong(y), (unsigned)deepest);  // wholes below the ceiling
     const double p = fma(fma(fma(fma(series.c4, f, c3), f, series.c2), f, series.c1), f, 1.0) * powers[below & (kPowersN - 1)];
     u64 w = Exp::fixed_of(__hiloint2double(__double2hiint(p) - (int)((below << 14) & 0xfff00000u), __double2loint(p)));
     if (masked && x == -INFINITY) w = 0;

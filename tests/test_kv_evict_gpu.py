@@ -50,7 +50,7 @@ def test_ragged_batch(dtype, heads, sink, recent):
     assert run(case, [5, 0, 15, 3, 16, 63, 1, 100, 299, 1024], sink=sink, recent=recent) > 100
 
 
-@pytest.mark.parametrize("n,keep", [(255, 1), (256, 255), (257, 128), (1000, 0), (1000, 999), (1000, 1000), (1000, 5000), (1000, -3), (2049, 1025), (7000, 3500), (20001, 10000), (32768, 30000), (40007, 25000)])
+@pytest.mark.parametrize("n,keep", [(255, 1), (256, 255), (257, 128), (1000, 0), (1000, 999), (1000, 1000), (1000, 5000), (1000, -3), (2049, 1025), (7000, 3500), (20001, 10000), (32768, 30000), (40007, 25000), (262144, 262100)])
 def test_lengths_across_the_sizes_of_the_search(n, keep):
     run(CacheCase([n, max(1, n // 3)], 1, 1, 64), [keep, keep // 3], sink=2, recent=min(20, n))
 
@@ -164,3 +164,10 @@ def test_refusals():
     torch.cuda.synchronize()
     case.ctx.check()
     assert case.got_records().tobytes() == case.records.tobytes()
+    roomy = CacheCase([20], 1, 1, 64, room=1 << 18)              # tables and a context for more than 2^18 tokens
+    with pytest.raises(hb.HarliError) as e:
+        roomy.evict([5], max_kv_len=(1 << 18) + 1)
+    assert e.value.status == hb.HARLI_ERR_INVALID and "above" in str(e.value)
+    roomy.evict([5], max_kv_len=1 << 18)
+    torch.cuda.synchronize()
+    roomy.ctx.check()

@@ -118,6 +118,38 @@ def test_masks_infinities_and_nan():
     assert check(z, r.random(12), temperature=np.full(12, np.nan))[0] == -1
 
 
+@pytest.mark.parametrize("offset", [3e3, -1e6, 1e8, -3e9, 2e11, -1e15])
+def test_logits_far_from_zero(offset):
+    """Floats lie up to thousands of units apart out there; a temperature of their distance makes neighbours worth telling apart."""
+    r = np.random.default_rng(3)
+    step = float(np.spacing(np.float32(abs(offset))))
+    z = (np.float32(offset) + np.float32(step) * r.integers(-6, 7, (12, 5000)).astype(np.float32)).astype(np.float32)
+    z[0, ::7], z[1, ::3], z[2, 5:] = np.finfo(np.float32).min, -np.inf, np.nan
+    for t in (0.03, 0.7, 5.0, step, step / 50, step * 40):
+        check(z, r.random(12), temperature=np.full(12, t))
+        check(z, r.random(12), temperature=np.full(12, t), top_k=np.full(12, 700), top_p=np.full(12, 0.9), min_p=np.full(12, 1e-4))
+
+
+def test_largest_vocabulary():
+    """2^20 tokens: spread out, and all alike (more tokens in one bin than are listed: the row itself is searched)."""
+    r = np.random.default_rng(5)
+    V = 1 << 20
+    z = np.stack([r.normal(0, 2.5, V).astype(np.float32), np.zeros(V, np.float32)])
+    check(z, [0.3, 0.7])
+    check(z, [0.9, 0.2], top_k=[50, 600000])
+    check(z, [0.6, 0.999], top_k=[1000, V - 1], min_p=[0.01, 0.5])
+    token, logprob = sample(z, [0.5, 0.5], top_p=[0.9, 0.25])
+    assert token[1] == V // 8 and logprob[1] == np.float32(-math.log(V // 4))    # half of the first quarter
+
+
+@pytest.mark.parametrize("spread", [0.01, 0.3, 1.0, 20.0])
+def test_flat_and_steep_rows_of_a_large_vocabulary(spread):
+    """Narrow rows have more tokens in a bin than are listed, wide ones cuts below the bins."""
+    z, r = rows(4, 50257, 11, spread)
+    check(z, r.random(4), top_k=[10, 1000, 20000, 50000], temperature=[0.05, 1.0, 1.0, 3.0])
+    check(z, r.random(4), min_p=[1e-9, 0.5, 0.9, 1e-4], temperature=[0.05, 1.0, 1.0, 3.0])
+
+
 @pytest.mark.parametrize("u", [0.0, -0.0, -1.0, float("nan"), 1.0, 2.0, float("inf"), np.nextafter(np.float32(1), np.float32(0)), 1e-30, 1e-45])
 def test_random_numbers_at_and_past_the_ends(u):
     z, r = rows(6, 900, 2)
