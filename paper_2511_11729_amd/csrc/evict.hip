@@ -125,22 +125,39 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
 #pragma unroll
     for (int u = 0; u < U; ++u) k[u] = good(pg[u]) ? rank_key(r[u], a.sink, recent_from) : 0;
   };
-  if constexpr (KEYS) {
-    constexpr int U = 8;
+  // the first pass of the search counts while the keys come in
+  constexpr int kTopDigit = 21;
+  auto clear = [&] {
+#pragma unroll
+    for (int i = 0; i < BPT; ++i) hist[tid * BPT + i] = 0;
+    __syncthreads();
+  };
+  clear();
+  {
+    constexpr int U = KEYS ? 8 : 4;
 #pragma unroll 1
     for (int t0 = tid; t0 < n; t0 += U * NT) {
       unsigned k[U];
       load_keys(t0, k);
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (t0 + u * NT < n) keys[t0 + u * NT] = k[u];
+        if (t0 + u * NT < n) {
+          if constexpr (KEYS) keys[t0 + u * NT] = k[u];
+          atomicAdd(&hist[kBins - 1 - (k[u] >> kTopDigit)], 1);  // the highest first
+        }
     }
   }
-  // f(token, key) for the tokens of this thread
+  // f(key) for the tokens of this thread
   auto each = [&](auto&& f) {
     if constexpr (KEYS) {
-#pragma unroll 4
-      for (int t = tid; t < n; t += NT) f(t, keys[t]);
+#pragma unroll 2
+      for (int t = 4 * tid; t < n; t += 4 * NT) {
+        const uint4 k = *reinterpret_cast<const uint4*>(keys + t);
+        f(k.x);
+        if (t + 1 < n) f(k.y);
+        if (t + 2 < n) f(k.z);
+        if (t + 3 < n) f(k.w);
+      }
     } else {
       constexpr int U = 4;
 #pragma unroll 1
@@ -149,7 +166,7 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
         load_keys(t, k);
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          if (t + u * NT < n) f(t + u * NT, k[u]);
+          if (t + u * NT < n) f(k[u]);
       }
     }
   };
@@ -165,14 +182,14 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
   unsigned prefix = 0, mask = 0;
   int want = keep, count = n;
 #pragma unroll 1
-  for (int shift = 21; keep > 0 && want < count && shift >= 0; shift = shift == 21 ? 10 : shift == 10 ? 0 : -1) {
+  for (int shift = kTopDigit; keep > 0 && want < count && shift >= 0; shift = shift == kTopDigit ? 10 : shift == 10 ? 0 : -1) {
     const unsigned digits = shift ? 2047u : 1023u;
-#pragma unroll
-    for (int i = 0; i < BPT; ++i) hist[tid * BPT + i] = 0;
-    __syncthreads();
-    each([&](int, unsigned k) {
-      if ((k & mask) == prefix) atomicAdd(&hist[kBins - 1 - ((k >> shift) & digits)], 1);  // the highest first
-    });
+    if (shift < kTopDigit) {
+      clear();
+      each([&](unsigned k) {
+        if ((k & mask) == prefix) atomicAdd(&hist[kBins - 1 - ((k >> shift) & digits)], 1);
+      });
+    }
     __syncthreads();
     int h[BPT], sum = 0, all;
 #pragma unroll
@@ -197,7 +214,7 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
   // ---- who stays: 64 tokens in a row are a ballot ---------------------------------------------------------------------------
   const int n_up = (n + 63) / 64 * 64;
   if (keep == 0 || want == count) {  // nothing, or all of the last ones
-#pragma unroll 2
+#pragma unroll 4
     for (int t = tid; t < n_up; t += NT) {
       const u64 m = __ballot(t < n && keep > 0 && (key_of(min(t, n - 1)) & mask) >= prefix);
       if (lane == 0) stays[t / 64] = m;
@@ -240,19 +257,19 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
 #pragma unroll 1
   for (int at = part * share; at < end; at += kMoves) {
     __syncthreads();
-#pragma unroll 2
-    for (int t = tid; t < n; t += NT) {  // (a wave: one word)
-      const int w = t / 64;
-      const u64 lower = (1ull << lane) - 1;
+    // an eighth of a word per thread
+#pragma unroll 1
+    for (int x = tid; x < 8 * words; x += NT) {
+      const int w = x / 8, up = 8 * (x & 7);
+      const u64 free = holes_of(w), moving = movers_of(w);
       const int2 before = sums[w];
-      const bool in = stays[w] >> lane & 1;
-      if (t < keep) {
-        const int i = before.x + (int)__popcll(~stays[w] & lower) - at;
-        if (!in && i >= 0 && i < kMoves) pairs[i].y = t;
-      } else {
-        const int i = before.y + (int)__popcll(movers_of(w) & lower) - at;
-        if (in && i >= 0 && i < kMoves) pairs[i].x = t;
-      }
+      auto list = [&](u64 all, int i, auto&& put) {
+        i += (int)__popcll(all & ((1ull << up) - 1)) - at;
+        for (unsigned bits = (unsigned)(all >> up) & 255; bits; bits &= bits - 1, ++i)
+          if (i >= 0 && i < kMoves) put(i, 64 * w + up + __ffs((int)bits) - 1);
+      };
+      list(free, before.x, [&](int i, int t) { pairs[i].y = t; });
+      list(moving, before.y, [&](int i, int t) { pairs[i].x = t; });
     }
     __syncthreads();
     const int n_moves = min(kMoves, end - at);
