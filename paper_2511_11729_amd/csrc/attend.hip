@@ -347,7 +347,7 @@ extern "C" harli_status harli_kv_attend(harli_ctx* c, const harli_attend_batch* 
   if (!b->q || !b->out || !b->n_tokens || !b->page_table) return fail(HARLI_ERR_INVALID, "kv_attend: q, out, n_tokens and page_table are required");
   if (((uintptr_t)b->q | (uintptr_t)b->out) % 16) return fail(HARLI_ERR_INVALID, "kv_attend: q and out have to be 16-byte aligned");
   if (b->max_kv_len < 1 || b->max_kv_len > m.max_seq_len) return fail(HARLI_ERR_INVALID, "kv_attend: max_kv_len %d outside 1..%d", b->max_kv_len, m.max_seq_len);
-  if (b->max_pages > kMostPages || b->max_pages * kPageTokens < b->max_kv_len)
+  if (b->max_pages > kMostPages || (long long)b->max_pages * kPageTokens < b->max_kv_len)
     return fail(HARLI_ERR_INVALID, "kv_attend: page table rows of %d pages cannot hold %d tokens", b->max_pages, b->max_kv_len);
   harli_status s = check_tracking(c, &b->track, b->batch, b->max_kv_len, "kv_attend");
   if (s != HARLI_OK) return s;
@@ -371,7 +371,7 @@ extern "C" harli_status harli_kv_record_init(harli_ctx* c, const harli_record_ba
   if (!b->n_tokens || !b->page_table || !b->records) return fail(HARLI_ERR_INVALID, "kv_record_init: n_tokens, page_table and records are required");
   if ((uintptr_t)b->records % 16) return fail(HARLI_ERR_INVALID, "kv_record_init: records are not 16-byte aligned");
   if (b->max_kv_len < 1 || b->max_kv_len > m.max_seq_len) return fail(HARLI_ERR_INVALID, "kv_record_init: max_kv_len %d outside 1..%d", b->max_kv_len, m.max_seq_len);
-  if (b->max_pages > kMostPages || b->max_pages * kPageTokens < b->max_kv_len)
+  if (b->max_pages > kMostPages || (long long)b->max_pages * kPageTokens < b->max_kv_len)
     return fail(HARLI_ERR_INVALID, "kv_record_init: page table rows of %d pages cannot hold %d tokens", b->max_pages, b->max_kv_len);
   const long long most = (long long)((b->max_kv_len + kPageTokens - 1) / kPageTokens) * m.n_kv_heads * kPageTokens;
   const int blocks = (int)((most + 255) / 256);

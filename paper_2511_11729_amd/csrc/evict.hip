@@ -377,7 +377,7 @@ extern "C" harli_status harli_kv_evict(harli_ctx* c, const harli_evict_batch* b,
     return fail(HARLI_ERR_INVALID, "kv_evict: n_tokens, keep, page_table and records are required");
   if ((uintptr_t)b->records % 16) return fail(HARLI_ERR_INVALID, "kv_evict: records are not 16-byte aligned");
   if (b->max_kv_len < 1 || b->max_kv_len > m.max_seq_len) return fail(HARLI_ERR_INVALID, "kv_evict: max_kv_len %d outside 1..%d", b->max_kv_len, m.max_seq_len);
-  if (b->max_pages > kMostPages || b->max_pages * kPageTokens < b->max_kv_len)
+  if (b->max_pages > kMostPages || (long long)b->max_pages * kPageTokens < b->max_kv_len)
     return fail(HARLI_ERR_INVALID, "kv_evict: page table rows of %d pages cannot hold %d tokens", b->max_pages, b->max_kv_len);
   if (b->sink < 0 || b->recent < 0) return fail(HARLI_ERR_INVALID, "kv_evict: sink %d, recent %d", b->sink, b->recent);
   if (b->n_left && (b->n_left == b->n_tokens || b->n_left == b->keep || b->n_left == b->position))

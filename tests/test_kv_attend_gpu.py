@@ -249,3 +249,17 @@ def test_refusals():
     torch.cuda.synchronize()
     case.ctx.check()
     assert bool((out == 7).all()) and torch.equal(before, case.track)
+
+
+@pytest.mark.parametrize("max_pages", [0, -1, 2 - (1 << 28), -(1 << 31)])
+def test_rows_of_no_pages_are_refused(max_pages):
+    # (2 - 2^28) * 16 is 32 in 32 bits
+    case = CacheCase([20, 30], 2, 2, 64)
+    q = torch.zeros(2, 2, 64, device=DEV)
+    keep = torch.tensor([5, 5], dtype=torch.int32, device=DEV)
+    table = dict(batch=2, n_tokens=case.n_dev, page_table=case.table_dev, max_pages=max_pages, max_kv_len=30, track=case.track)
+    for call in (lambda: case.ctx.kv_attend(layer=0, q=q, out=torch.empty_like(q), workspace=case.workspace, **table),
+                 lambda: case.ctx.kv_record_init(**table), lambda: case.ctx.kv_evict(keep=keep, **table)):
+        with pytest.raises(hb.HarliError) as e:
+            call()
+        assert e.value.status == hb.HARLI_ERR_INVALID
