@@ -261,7 +261,7 @@ class DecodeServer:
                         raise
                     # the reserve is there to prevent this; if it happens the sequence goes back to the queue
                     self.preempted += 1
-                    self.queue.appendleft((seq[1], seq[2]))
+                    self.queue.appendleft((seq[3], seq[2]))   # (as a prompt of all tokens it has had, those that left its cache too)
                     self._drop(b, done)
                     continue
             b += 1

@@ -269,3 +269,25 @@ def test_service_inside_a_budget_gives_pages_back():
     for s in (dict(keep=0), dict(keep=5, slack=0)):
         with pytest.raises(ValueError):
             serving(budget=serve.KvBudget(**s))
+
+
+def test_a_sequence_that_is_sent_back_returns_with_all_tokens_it_has_had():
+    args, w, m, ft, pool, ctx, ft_step, sizes, keep = small()
+    server = serve.DecodeServer(ctx, pool, m, max_batch=2, max_len=args.max_len, stream=torch.cuda.Stream(), slab=keep[0],
+                                budget=serve.KvBudget(keep=40, slack=16, sink=2, recent=8))
+    server.submit([(60, 40)])
+    server.step()[0].synchronize()
+    assert server.running[0][1:4] == [40, 39, 61] and server.evicted == 21     # cached, left, had
+    alloc = pool.alloc_pages
+
+    def none_left(n):
+        raise hb.HarliError(hb.HARLI_ERR_OOM, "none left")
+    pool.alloc_pages = none_left                       # the page for a 49th token
+    for _ in range(8):
+        server.step()[0].synchronize()
+    assert server.preempted == 1 and not server.running and list(server.queue) == [(69, 31)]
+    pool.alloc_pages = alloc
+    server.step()[0].synchronize()
+    assert server.running[0][1:4] == [40, 30, 70]      # its next token has position 69
+    ctx.check(server.stream)
+    server.drain()
