@@ -479,6 +479,8 @@ def adamw_step(master, m, v, grad, param_bf16, *, step: int, lr=1e-3, beta1=0.9,
 def sample(logits, uniform, token, *, workspace, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, stream=None) -> None:
     """A token per row of logits (fp32 [batch, vocab], rows may lie apart) from the random numbers `uniform`; the settings are device
     tensors [batch] or None.  workspace: sample_workspace_bytes(batch, vocab) bytes on the device."""
+    if logits.dim() != 2 or str(logits.dtype) != "torch.float32" or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("sample: logits have to be fp32 [batch, vocab], a row's side by side")
     b = SampleBatch(logits.shape[0], logits.shape[1], _ptr(logits), logits.stride(0), _ptr(uniform), _ptr(temperature), _ptr(top_k),
                     _ptr(top_p), _ptr(min_p), _ptr(token), _ptr(logprob), _ptr(workspace), workspace.numel() * workspace.element_size())
     _check(lib().harli_sample(C.byref(b), _stream(stream)))

@@ -98,6 +98,8 @@ class DecodeServer:
         if budget is not None:
             if budget.keep < 1 or budget.slack < 1:
                 raise ValueError("a budget keeps at least one token and cuts at least one")
+            if max_len > 1 << 18:
+                raise ValueError("a budget is for sequences of at most 2^18 tokens (harli_kv_evict)")
             st = pool.stats()
             self.track = torch.zeros(pool.cfg.n_layers, st.n_chunks * st.pages_per_block, m.n_kv, P, 2, dtype=torch.int32, device=dev)
             self.attend_ws = torch.empty(ctx.kv_attend_workspace_bytes(max_batch, max_len), dtype=torch.uint8, device=dev)

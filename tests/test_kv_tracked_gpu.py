@@ -291,3 +291,9 @@ def test_a_sequence_that_is_sent_back_returns_with_all_tokens_it_has_had():
     assert server.running[0][1:4] == [40, 30, 70]      # its next token has position 69
     ctx.check(server.stream)
     server.drain()
+
+
+def test_a_budget_for_longer_sequences_than_an_eviction_takes_is_refused():
+    args, w, m, ft, pool, ctx, ft_step, sizes, keep = small()
+    with pytest.raises(ValueError):
+        serve.DecodeServer(ctx, pool, m, max_batch=1, max_len=(1 << 18) + 1, stream=torch.cuda.Stream(), budget=serve.KvBudget(keep=40))

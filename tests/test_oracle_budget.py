@@ -87,3 +87,11 @@ def test_cache_calls_refuse_a_null_context():
         refused("null", getattr(l, name), None, ctypes.byref(cls()), None)
     refused("null", l.harli_decode_step_tracked, None, None, None, None)
     assert l.harli_kv_attend_workspace_bytes(None, 1, 1) == 0
+
+
+def test_logits_that_are_not_rows_of_fp32_are_refused():
+    torch = pytest.importorskip("torch")
+    z = torch.zeros(4, 6)
+    for bad in (z.t(), z[:, ::2], z.double(), z[0], z[None]):
+        with pytest.raises(ValueError):
+            hb.sample(bad, z, z, workspace=z)
