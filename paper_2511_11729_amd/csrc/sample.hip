@@ -247,7 +247,7 @@ constexpr int kListed = kCandidates / kRowWaves;   // tokens of the bin a wave c
 struct RowShared {
   u64 digit[kDigits];
   double powers[kPowersN];
-  uint2 listed[kCandidates];      // (logit's bits, index); then (key, index)
+  uint2 listed[kCandidates];      // (key, index)
   float top[kMostStretches];
   int below[kMostStretches];      // bins from the row's first to the stretch's
   double scale[kMostStretches];   // of the stretch's sums to the row's, which are relative to its largest logit
@@ -520,31 +520,49 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
         };
         float v[R], ahead[R];
         int lo = needed(wave * kPart);
+        auto fetch = [&] {
+          const float* p = z + lo;  // (the same in all lanes)
+          if (lo + kPart <= V) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) ahead[r] = z[min(lo + r * 64 + lane, V - 1)];
+            for (int r = 0; r < R; ++r) ahead[r] = p[r * 64 + (unsigned)lane];
+          } else if (lo < V) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) ahead[r] = r * 64 + lane < V - lo ? p[r * 64 + lane] : NAN;
+          }
+        };
+        fetch();
 #pragma unroll 1
-        while (lo < V) {
+        while (lo < V && listed <= kListed) {
           const int now = lo;
           lo = needed(now + kRowWaves * kPart);
 #pragma unroll
           for (int r = 0; r < R; ++r) v[r] = ahead[r];
-          if (lo < V) {
+          fetch();
+          // a bit per token of the lane; then every lane lists its own
+          unsigned hits = 0;
 #pragma unroll
-            for (int r = 0; r < R; ++r) ahead[r] = z[min(lo + r * 64 + lane, V - 1)];
-          }
-#pragma unroll
-          for (int r = 0; r < R; ++r) {
-            const bool in = v[r] >= border[0] && v[r] < border[1] && lane < V - now - r * 64;
-            const u64 who = __ballot(in);
-            if (who) {
-              const int at = listed + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(who >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)who, 0u));
-              if (in && at < kListed) sh.listed[wave * kListed + at] = make_uint2(__float_as_uint(v[r]), (unsigned)(now + r * 64 + lane));
-              listed += __popcll(who);
-            }
+          for (int r = R - 1; r >= 0; --r) hits = hits + hits + (v[r] >= border[0] && v[r] < border[1]);
+          const int n = __popc(hits), upto = wave_scan(n), all = lane_value(upto, 63);
+          int at = wave * kListed + listed + upto - n;
+          listed += all;
+          if (listed <= kListed) {
+#pragma unroll 1
+            for (; hits; hits &= hits - 1, ++at) sh.listed[at].y = (unsigned)(now + lane + 64 * (__ffs((int)hits) - 1));
           }
         }
         if (listed > kListed && lane == 0) sh.overflow = 1;
-        for (int i = lane; i < min(listed, kListed); i += 64) sh.listed[wave * kListed + i].x = order_key(__uint_as_float(sh.listed[wave * kListed + i].x));
+        if (listed <= kListed) {  // their keys
+          constexpr int U = 4;
+#pragma unroll 1
+          for (int i = lane; i < listed; i += U * 64) {
+            float x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[u] = z[sh.listed[wave * kListed + min(i + u * 64, listed - 1)].y];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+              if (i + u * 64 < listed) sh.listed[wave * kListed + i + u * 64].x = order_key(x[u]);
+          }
+        }
         __syncthreads();
       }
       in_lds = bin < kLogitBins && sh.overflow == 0;
