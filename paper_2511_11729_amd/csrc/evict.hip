@@ -44,8 +44,6 @@ __device__ __forceinline__ int scan_before(int v, int* tmp, int lane, int wave, 
 struct EvictArgs {
   harli_evict_batch b;
   int n_kv, row_bytes, row_lanes;  // row_lanes: the power of two of lanes that move a row, words of it each
-  int parts;                       // workgroups per (layer, sequence, KV head): each moves rows of its own
-  bool rows, records;              // what this launch moves
   char* slab;
   KvGeom geom;
   int* err_flag;
@@ -63,6 +61,8 @@ size_t evict_lds(int max_kv_len, bool keys, int threads) {
 }
 
 // NT threads; KEYS: the keys stay in LDS; rows move in words of VEC bytes.
+// One workgroup per head, also for few long sequences: several of them that share a head's rows need a second launch for the records that
+// all go by (two of 30003 cut to an eighth, 64 heads: 114 us instead of 127; but two of 12000 that give up 16 tokens 37 instead of 21).
 // The time goes into the rows at large sizes, and into latencies and the kernel's own code at small ones, hence loops instead of unrolled
 // rounds over keys in registers (39 KB of code: 21.6 us for 16 sequences that give up one page of 1040 tokens in eight layers).
 template <int NT, bool KEYS, int VEC>
@@ -72,10 +72,10 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
   const harli_evict_batch& a = args.b;
   const KvGeom& geom = args.geom;
   const int n_kv = args.n_kv;
-  const int c = blockIdx.x / args.parts, part = blockIdx.x - c * args.parts, b = blockIdx.y, layer = blockIdx.z;
+  const int c = blockIdx.x, b = blockIdx.y, layer = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = a.n_tokens[b], keep = max(a.keep[b], 0);
-  const bool first = c == 0 && layer == 0 && part == 0;
+  const bool first = c == 0 && layer == 0;
   if (n > a.max_kv_len || n > a.max_pages * kPageTokens) {
     if (first && tid == 0) {
       atomicOr(args.err_flag, 4);
@@ -253,9 +253,8 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
   }
   typedef unsigned int __attribute__((ext_vector_type(VEC / 4))) word;
   const int row_words = args.row_bytes / VEC, row_lanes = args.row_lanes, per_pass = NT / row_lanes, x0 = tid & (row_lanes - 1), r0 = tid / row_lanes;
-  const int share = (total + args.parts - 1) / args.parts, end = min(total, (part + 1) * share);
 #pragma unroll 1
-  for (int at = part * share; at < end; at += kMoves) {
+  for (int at = 0; at < total; at += kMoves) {
     __syncthreads();
     // an eighth of a word per thread
 #pragma unroll 1
@@ -272,7 +271,7 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
       list(moving, before.y, [&](int i, int t) { pairs[i].x = t; });
     }
     __syncthreads();
-    const int n_moves = min(kMoves, end - at);
+    const int n_moves = min(kMoves, total - at);
 #pragma unroll 1
     for (int i = tid; i < n_moves; i += NT) {
       const int src = pairs[i].x, dst = pairs[i].y;
@@ -283,10 +282,9 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
         return kv_page_off(geom, page, layer, 0) + (size_t)(c * kPageTokens + slot % kPageTokens) * args.row_bytes;
       };
       moves[i] = ok ? Move{row_off(ps, src), row_off(pd, dst)} : Move{0, 0};  // (to itself)
-      if (ok && args.records) rec[pd * page_recs + dst % kPageTokens] = rec[ps * page_recs + src % kPageTokens];
+      if (ok) rec[pd * page_recs + dst % kPageTokens] = rec[ps * page_recs + src % kPageTokens];
     }
     __syncthreads();
-    if (!args.rows) continue;
     // keys and values of four rows in flight
     constexpr int U = 4;
 #pragma unroll 1
@@ -336,31 +334,22 @@ harli_status launch_evict(EvictArgs a, int heads, int layers, int n_cu, hipStrea
   const int n = a.b.max_kv_len, words = a.row_bytes / VEC;
   for (a.row_lanes = 1; a.row_lanes < words && a.row_lanes < 64;) a.row_lanes *= 2;
   const bool keys = n <= kKeysInLds;
-  const int threads = n <= 2048 ? 256 : n <= 16384 ? 512 : 1024;
+  // Threads of a workgroup: as many as let every head run at once (2048 threads per CU), not more than the length has work for, and
+  // 1024 where the keys leave a CU's LDS to one workgroup.  256 / 512 / 1024 threads in us, 16 tokens leave: 1024 heads of 1000 tokens
+  // 16.9 / 22.1 / 38.1, of 4000 35.3 / 38.4 / 53.9, of 8000 66.9 / 57.7 / 70.0; 512 heads of 1000 13.6 / 14.1 / 21.4, of 16000
+  // 62.2 / 53.1 / 58.8; 64 heads of 1000 10.3 / 10.3 / 11.5, of 4000 14.8 / 12.0 / 12.6, of 16000 35.9 / 23.7 / 19.6.
+  const long long all = (long long)heads * layers * a.b.batch;
+  const int threads = n > 16384 || (all <= n_cu && n > 4096) ? 1024 : all <= 2 * n_cu || n > 2048 ? 512 : 256;
   const size_t lds = evict_lds(n, keys, threads);
   if (lds > (48u << 10)) {  // (with the kernel's own)
     const harli_status rc = allow_evict_lds();
     if (rc != HARLI_OK) return rc;
   }
-  auto go = [&](bool rows, bool records) {
-    a.rows = rows, a.records = records;
-    if (!rows) a.parts = 1;
-    const dim3 grid(heads * a.parts, a.b.batch, layers);
-    if (threads == 256) hipLaunchKernelGGL((k_evict<256, true, VEC>), grid, dim3(256), lds, st, a);
-    else if (threads == 512) hipLaunchKernelGGL((k_evict<512, true, VEC>), grid, dim3(512), lds, st, a);
-    else if (keys) hipLaunchKernelGGL((k_evict<1024, true, VEC>), grid, dim3(1024), lds, st, a);
-    else hipLaunchKernelGGL((k_evict<1024, false, VEC>), grid, dim3(1024), lds, st, a);
-  };
-  // Few long sequences: several workgroups find the same moves and share the rows.  The records they go by must not change
-  // meanwhile, so those move in a launch of their own.
-  const long long heads_all = (long long)heads * layers * a.b.batch;
-  a.parts = n > 2048 ? (int)std::max(1ll, std::min(8ll, n_cu / heads_all)) : 1;
-  if (a.parts == 1) {
-    go(true, true);
-  } else {
-    go(true, false);
-    go(false, true);
-  }
+  const dim3 grid(heads, a.b.batch, layers);
+  if (threads == 256) hipLaunchKernelGGL((k_evict<256, true, VEC>), grid, dim3(256), lds, st, a);
+  else if (threads == 512) hipLaunchKernelGGL((k_evict<512, true, VEC>), grid, dim3(512), lds, st, a);
+  else if (keys) hipLaunchKernelGGL((k_evict<1024, true, VEC>), grid, dim3(1024), lds, st, a);
+  else hipLaunchKernelGGL((k_evict<1024, false, VEC>), grid, dim3(1024), lds, st, a);
   return HARLI_OK;
 }
 
