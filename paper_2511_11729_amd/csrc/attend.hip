@@ -17,10 +17,12 @@ namespace {
 
 constexpr int kPageTokens = 16;
 constexpr int kMostPages = 1 << 26;  // of a table row: token indexes stay in 32 bits
-constexpr int kChunkF32 = 256;    // tokens per chunk on fp32 storage: one per thread
+constexpr int kChunkF32 = 256;       // tokens per chunk on fp32 storage: one per thread
 constexpr int kFinishTokens = 1024;  // tokens of a block of records: four per thread
 constexpr int kPiece = 64;           // elements of an output row that are joined at a time
-constexpr int kFewChunks = 16;       // up to here an output element is one thread's
+// up to here an output element is one thread's (64 sequences of 200 tokens, 28 / 4 heads: 20.3 us instead of 23.6; 16 of 4096, 32 chunks,
+// 32 / 8 heads: 84.0 instead of 83.2)
+constexpr int kFewChunks = 16;
 
 // fp32 storage: one chunk of one query head; a thread scores one token, then a wave adds up P.V of every fourth token with a lane
 // per element.  EL: elements per lane; a head larger than 64 EL goes to several workgroups (blockIdx.z), which score it alike.
@@ -128,7 +130,8 @@ __global__ void __launch_bounds__(256) k_attend_finish(FinishArgs a, AttendWs at
   __shared__ float red[256 * VEC];
   constexpr int HP = 8;  // query heads whose scores are fetched ahead
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int part = blockIdx.x / a.n_kv, c = blockIdx.x - part * a.n_kv, G = a.n_q / a.n_kv;
+  // (turned from sequence to sequence: the first parts have the most to do, and every eighth workgroup goes to the same XCD)
+  const int at_x = (blockIdx.x + b) % gridDim.x, part = at_x / a.n_kv, c = at_x - part * a.n_kv, G = a.n_q / a.n_kv;
   const int n = max(0, min(min(a.kv_len[b] + att.n_new, att.n_chunks * att.chunk), a.max_pages * kPageTokens));
   const int nch = (n + att.chunk - 1) / att.chunk;
   const size_t head0 = (size_t)b * a.n_q + c * G;
@@ -316,10 +319,13 @@ void attend_f32(harli_ctx* c, const float* q, const int* kv_len, const int* page
 void attend_finish(harli_ctx* c, const AttendWs& att, const int* kv_len, const int* page_table, int batch, int max_pages, int layer,
                    float* out, unsigned short* frag, const harli_tracking* t, hipStream_t st) {
   const harli_model_cfg& m = c->cfg;
-  // Enough workgroups for the chip, as far as there is work for them: blocks of records and pieces of rows.
+  // Workgroups of a KV head: one per block of records as far as the chip holds them, and for the output rows two per CU.  In us for the
+  // whole call, bf16, heads of 128: 32 sequences of about 3000 tokens, 28 / 4 heads, 1 / 4 / as many parts as there are blocks (8):
+  // 66.3 / 61.4 / 58.9; one of 32001, 32 / 8 heads, 1 / 4 / 32: 50.7 / 50.2 / 50.0.  Output rows with one / two / four / sixteen
+  // workgroups per CU: 16 of 1024, 32 / 8 heads, 30.4 / 31.1 / 33.5 / 33.0; 64 of 200, 28 / 4 heads, 21.1 / 20.3 / 21.2 / 25.1.
   const int G = m.n_q_heads / m.n_kv_heads, blocks = att.scores ? (att.score_ld + kFinishTokens - 1) / kFinishTokens : 0;
-  const int most = std::max(blocks, G * ((m.head_dim + kPiece - 1) / kPiece));
-  const int parts = std::max(1, std::min(most, 16 * c->n_cu / (batch * m.n_kv_heads)));
+  const int pieces = G * ((m.head_dim + kPiece - 1) / kPiece), heads = batch * m.n_kv_heads;
+  const int parts = std::max({1, std::min(blocks, 16 * c->n_cu / heads), std::min(pieces, 2 * c->n_cu / heads)});
   const FinishArgs a{kv_len, page_table, t->position, max_pages, layer, m.n_q_heads, m.n_kv_heads, m.head_dim, c->geom.n_pages_total, parts,
                      out, frag, t->records, t->decay};
   const dim3 grid(m.n_kv_heads * parts, batch);
