@@ -285,8 +285,8 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
       if (ok) rec[pd * page_recs + dst % kPageTokens] = rec[ps * page_recs + src % kPageTokens];
     }
     __syncthreads();
-    // keys and values of four rows in flight
-    constexpr int U = 4;
+    // keys and values of several rows in flight: eight where a head has a CU to itself (two of 30003, 128 heads: 143.7 us, four 147.2)
+    constexpr int U = NT == 1024 ? 8 : 4;
 #pragma unroll 1
     for (int i = r0; i < n_moves; i += U * per_pass)
 #pragma unroll 1
@@ -336,7 +336,8 @@ harli_status launch_evict(EvictArgs a, int heads, int layers, int n_cu, hipStrea
   const bool keys = n <= kKeysInLds;
   // Threads of a workgroup: as many as let every head run at once (2048 threads per CU), not more than the length has work for, and
   // 1024 where the keys leave a CU's LDS to one workgroup.  256 / 512 / 1024 threads in us, 16 tokens leave: 1024 heads of 1000 tokens
-  // 16.9 / 22.1 / 38.1, of 4000 35.3 / 38.4 / 53.9, of 8000 66.9 / 57.7 / 70.0; 512 heads of 1000 13.6 / 14.1 / 21.4, of 16000
+  // 16.9 / 22.1 / 38.1, of 4000 35.3 / 38.4 / 53.9, of 8000 66.9 / 57.7 / 70.0 (3072 of about 800, the longest 3076, cut to half:
+  // 187 / 178 / -); 512 heads of 1000 13.6 / 14.1 / 21.4, of 16000
   // 62.2 / 53.1 / 58.8; 64 heads of 1000 10.3 / 10.3 / 11.5, of 4000 14.8 / 12.0 / 12.6, of 16000 35.9 / 23.7 / 19.6.
   const long long all = (long long)heads * layers * a.b.batch;
   const int threads = n > 16384 || (all <= n_cu && n > 4096) ? 1024 : all <= 2 * n_cu || n > 2048 ? 512 : 256;
