@@ -1,6 +1,8 @@
 // Eviction from the paged KV cache by accumulated attention weight (harli_kv_evict).  Every (layer, sequence, KV head) ranks its
 // own tokens, keeps the best and moves those of them that lie behind the kept length into the slots that fell free.
-// Reads 8 bytes per token and moves whole rows of keys and values: bound by HBM.  Only rows behind the kept length move (not
+// Reads 8 bytes per token and moves whole rows of keys and values: bound by HBM where many rows move (192 sequences of about 800 tokens
+// cut to half, 759 MB in 167 us: 4.5 TB/s, a large copy reaches 4.7), by latency where few do (16 of 1040 tokens that give up a page,
+// 128 heads each: 13.7 us for 26 MB).  Only rows behind the kept length move (not
 // everything behind the first gap, as keeping the order would): a service that gives up one page of 16 tokens at a time moves at
 // most 16 rows per head, and sources (slots >= keep) and targets (slots < keep) never meet, so rows move in any order.
 #include <algorithm>
@@ -17,7 +19,9 @@ constexpr int kPageTokens = 16;
 constexpr int kMostPages = 1 << 26;  // of a table row: token indexes stay in 32 bits
 constexpr int kMostTokens = 1 << 18;  // of a sequence: a bit each in LDS
 constexpr int kBins = 2048;           // of the search for the last weight that stays: 11, 11 and 10 bits
-constexpr int kKeysInLds = 32768;     // tokens whose keys are read once and stay in LDS; of longer sequences they are read again for every pass
+// Tokens whose keys are read once and stay in LDS (128 KiB of a CU's 160); of longer sequences they are read again for every pass.  Two of
+// 30003 in 128 heads, cut to an eighth / giving up 16 tokens: 143 / 34 us, read again 174 / 52.
+constexpr int kKeysInLds = 32768;
 
 // Order of the weights as unsigned integers: NaN below every other, both zeros alike, protected tokens above.
 __device__ __forceinline__ unsigned rank_key(uint2 rec, int sink, long long recent_from) {
@@ -64,7 +68,8 @@ size_t evict_lds(int max_kv_len, bool keys, int threads) {
 // One workgroup per head, also for few long sequences: several of them that share a head's rows need a second launch for the records that
 // all go by (two of 30003 cut to an eighth, 64 heads: 114 us instead of 127; but two of 12000 that give up 16 tokens 37 instead of 21).
 // The time goes into the rows at large sizes, and into latencies and the kernel's own code at small ones, hence loops instead of unrolled
-// rounds over keys in registers (39 KB of code: 21.6 us for 16 sequences that give up one page of 1040 tokens in eight layers).
+// rounds over keys in registers (39 KB of code: 21.6 us where the loops took 17.5, for 16 sequences of 1040 tokens that give up one page
+// in eight layers).
 template <int NT, bool KEYS, int VEC>
 __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
   constexpr int NW = NT / 64, BPT = kBins / NT, kMoves = moves_listed(NT);
@@ -336,8 +341,8 @@ harli_status launch_evict(EvictArgs a, int heads, int layers, int n_cu, hipStrea
   const bool keys = n <= kKeysInLds;
   // Threads of a workgroup: as many as let every head run at once (2048 threads per CU), not more than the length has work for, and
   // 1024 where the keys leave a CU's LDS to one workgroup.  256 / 512 / 1024 threads in us, 16 tokens leave: 1024 heads of 1000 tokens
-  // 16.9 / 22.1 / 38.1, of 4000 35.3 / 38.4 / 53.9, of 8000 66.9 / 57.7 / 70.0 (3072 of about 800, the longest 3076, cut to half:
-  // 187 / 178 / -); 512 heads of 1000 13.6 / 14.1 / 21.4, of 16000
+  // 16.9 / 22.1 / 38.1, of 4000 35.3 / 38.4 / 53.9, of 8000 66.9 / 57.7 / 70.0 (16 each in 192 uneven sequences of about 800
+  // tokens cut to half: 187 / 178 / -); 512 heads of 1000 13.6 / 14.1 / 21.4, of 16000
   // 62.2 / 53.1 / 58.8; 64 heads of 1000 10.3 / 10.3 / 11.5, of 4000 14.8 / 12.0 / 12.6, of 16000 35.9 / 23.7 / 19.6.
   const long long all = (long long)heads * layers * a.b.batch;
   const int threads = n > 16384 || (all <= n_cu && n > 4096) ? 1024 : all <= 2 * n_cu || n > 2048 ? 512 : 256;

@@ -9,8 +9,9 @@
 //                     number points at, and the token in it.
 // Weights are exp in 64 bits rounded to fixed point, so sums by atomics are the same in any order; stretches are joined in 64-bit floating
 // point in a fixed order.  A row's result depends neither on the batch nor on scheduling.
-// What bounds it: HBM for the logits in the first launch, with the exponential in 64 bits close behind it (20 instructions per token: 20 us for
-// 256 rows of 152064 against 26 us of reading); in the second the latency of its steps.
+// What bounds it, 256 rows of 152064 logits: the first launch reads them in 25.3 us (6.2 TB/s) when it takes the maximum alone; the
+// exponential in 64 bits makes that 40.7, the bins 48.  The second takes 43, most of it for the tokens of the cut's bin: nearly every
+// stretch has some and is read again.  One row of 32000: 5.4 and 19 us, latency and a cold instruction cache.
 #include <mutex>
 
 #include "ctx.h"
@@ -20,7 +21,9 @@
 namespace harli {
 namespace {
 
-constexpr int kStretch = 4096;      // tokens per workgroup of the first launch: 16 per thread
+// tokens per workgroup of the first launch: 16 per thread (8192, half the bins to write and join: no gain there, the row's launch slower,
+// 128 rows of 128256 28.2 us instead of 24.6)
+constexpr int kStretch = 4096;
 constexpr int kMostVocab = 1 << 20;
 constexpr int kMostStretches = kMostVocab / kStretch;
 constexpr int kLogitBins = 256;     // of a stretch, downwards from its maximum
@@ -176,8 +179,8 @@ __global__ void __launch_bounds__(kStretchThreads) k_sample_stretch(harli_sample
   const bool far = !(fabs(ceiling) < kFarStretch);
   u64 sum = 0;
   unsigned count = 0;
-  // Logits below the bins and below all weights (2^-60) are taken as the one at that border, or the next below it that is a float.  This is the loop that the launch's time
-  // goes into: conversions between 64-bit floating point and integers, and ldexp, are slow beside sums and products, hence the sums beside
+  // Logits below the bins and below all weights (2^-60) are taken as the one at that border, or the next below it that is a float.
+  // This is the loop that the launch's time goes into: conversions between 64-bit floating point and integers, and ldexp, are slow beside sums and products, hence the sums beside
   // kWholes and the exponent added as bits.
   const int deepest = max(60 * 64, kLogitBins << shift) + 64;  // wholes; 2^-513 at most
   const double border = (ceiling - (double)deepest) / per_t;
@@ -481,7 +484,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
         if (tid < kLogitBins && sh.upto_weight[tid] >= want_d) atomicMin(&sh.found, (unsigned)tid);
         __syncthreads();
         bin = sh.found;
-            } else {  // the cut's own bin, for the last of equal logits and for the weights
+      } else {  // the cut's own bin, for the last of equal logits and for the weights
         if (s.min_p > 0.0) {
           const unsigned hi = smallest_key([&](unsigned k) { return ex.weight(order_value(k), top, per_t) >= s.min_p; },
                                            top + s.t * logf((float)s.min_p), order_key(top), lane);
