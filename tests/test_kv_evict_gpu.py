@@ -171,3 +171,14 @@ def test_refusals():
     roomy.evict([5], max_kv_len=1 << 18)
     torch.cuda.synchronize()
     roomy.ctx.check()
+
+
+# workgroups get smaller with more heads than the chip holds of the larger ones (above two per compute unit), by length
+@pytest.mark.parametrize("dtype,heads,layers,lengths", [("bf16", (8, 8, 64), 8, [0, 1, 16, 17, 255, 256, 300, 700, 1040]),
+                                                        ("f32", (40, 40, 6), 2, [2048, 2000, 3, 900, 100, 64, 63, 1]),
+                                                        ("f32", (40, 40, 4), 8, [12000, 2500]),
+                                                        ("f32", (40, 40, 4), 4, [6000, 4097])])
+def test_many_heads(dtype, heads, layers, lengths):
+    case = CacheCase(lengths, *heads, dtype=dtype, layers=layers)
+    assert heads[1] * layers * len(lengths) > 256
+    assert run(case, [(2 * n + 2) // 3 for n in lengths], sink=2, recent=8) > 1000
