@@ -323,8 +323,9 @@ void attend_finish(harli_ctx* c, const AttendWs& att, const int* kv_len, const i
   const harli_model_cfg& m = c->cfg;
   // Workgroups of a KV head: one per block of records as far as the chip holds them, and for the output rows two per CU.  In us for the
   // whole call, bf16, heads of 128: 32 sequences of about 3000 tokens, 28 / 4 heads, 1 / 4 / as many parts as there are blocks (8):
-  // 66.3 / 61.4 / 58.9; one of 32001, 32 / 8 heads, 1 / 4 / 32: 50.7 / 50.2 / 50.0.  Output rows with one / two / four / sixteen
-  // workgroups per CU: 16 of 1024, 32 / 8 heads, 30.4 / 31.1 / 33.5 / 33.0; 64 of 200, 28 / 4 heads, 21.1 / 20.3 / 21.2 / 25.1.
+  // 66.3 / 61.4 / 58.9; 192 of about 800, the longest 3076, 1 / 2 / 4: 120 / 111 / 109; one of 32001, 32 / 8 heads, 1 / 4 / 32: 50.7 /
+  // 50.2 / 50.0.  Output rows with one / two / four / sixteen workgroups per CU: 16 of 1024, 32 / 8 heads, 30.4 / 31.1 / 33.5 / 33.0;
+  // 64 of 200, 28 / 4 heads, 21.1 / 20.3 / 21.2 / 25.1.
   const int G = m.n_q_heads / m.n_kv_heads, blocks = att.scores ? (att.score_ld + kFinishTokens - 1) / kFinishTokens : 0;
   const int pieces = G * ((m.head_dim + kPiece - 1) / kPiece), heads = batch * m.n_kv_heads;
   const int parts = std::max({1, std::min(blocks, 16 * c->n_cu / heads), std::min(pieces, 2 * c->n_cu / heads)});
