@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(256) k_attend_finish(FinishArgs a, AttendWs at
 
   // ---- records
 #pragma unroll 1
-  for (; record && t - tid * 4 < n;) {
+  while (record && t - tid * 4 < n) {  // (fetch moves t)
     if (t < n && page >= 0 && page < a.n_pages) {  // (another page id is reported where its keys were asked for)
       harli_kv_record* rec = record_at();
       r[0] = reinterpret_cast<const uint4*>(rec)[0], r[1] = reinterpret_cast<const uint4*>(rec)[1];

@@ -29,7 +29,8 @@ __device__ __forceinline__ unsigned rank_key(uint2 rec, int sink, long long rece
   const unsigned u = __float_as_uint(__uint_as_float(rec.x) + 0.f);
   unsigned k = u & 0x80000000u ? ~u : u | 0x80000000u;
   k = (u & 0x7fffffffu) > 0x7f800000u ? 0 : k;
-  return (pos < sink) | ((long long)pos >= recent_from) ? 0xffffffffu : k;
+  const bool is_protected = (pos < sink) | ((long long)pos >= recent_from);
+  return is_protected ? 0xffffffffu : k;
 }
 
 // Sum of v over the threads before this one, and of all of them in `all` (the whole workgroup calls it; `tmp`: one entry per wave).
@@ -219,7 +220,6 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs args) {
   // ---- who stays: 64 tokens in a row are a ballot ---------------------------------------------------------------------------
   const int n_up = (n + 63) / 64 * 64;
   if (keep == 0 || want == count) {  // nothing, or all of the last ones
-#pragma unroll 4
     for (int t = tid; t < n_up; t += NT) {
       const u64 m = __ballot(t < n && keep > 0 && (key_of(min(t, n - 1)) & mask) >= prefix);
       if (lane == 0) stays[t / 64] = m;
