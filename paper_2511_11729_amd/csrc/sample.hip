@@ -263,7 +263,6 @@ struct RowShared {
   unsigned part_n[kRowThreads / kLogitBins][kLogitBins];
   u64 tmp[kRowWaves];
   float wave_f[kRowWaves];
-  unsigned wave_u[2 * kRowWaves];
   u64 found_above;
   unsigned found;
   int least;
@@ -293,11 +292,11 @@ __device__ __forceinline__ T all_sum(T v, RowShared& sh, int lane, int wave) {
 
 // Among the items i = from, from + step, .. < end of every thread, key(i) and amount(i) (0: not looked at): the key at which the amounts of
 // higher keys are less than `want` and with its own not; `want` becomes what is missing above it (a want beyond the whole counts as the
-// whole).  Keys agree with `common` from bit `bits` on.
+// whole).  Keys are below 2^bits.
 template <typename Key, typename Amount>
-__device__ __forceinline__ unsigned find_key(int from, int end, int step, unsigned common, int bits, Key key, Amount amount, u64& want, RowShared& sh,
+__device__ __forceinline__ unsigned find_key(int from, int end, int step, int bits, Key key, Amount amount, u64& want, RowShared& sh,
                                              int tid, int lane, int wave) {
-  unsigned prefix = bits < 32 ? common >> bits << bits : 0;
+  unsigned prefix = 0;
 #pragma unroll 1
   while (bits > 0) {
     const int width = min(bits, 11), shift = bits - width;
@@ -417,6 +416,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
   unsigned t_key = 0, last = 0xffffffffu;
   int held = -1;  // the bin whose tokens are in LDS, and this wave's number of them
   int listed = 0;
+  unsigned bin_first = 0, bin_keys = 0;  // its smallest key, and how many there are to the next bin's
   bool in_lds = false;
   if (s.cut) {
     if (far) {
@@ -511,10 +511,13 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
         __syncthreads();
         // the logits of the bin: from the smallest in it (or above) to the smallest above it
         float border[2];
+        unsigned border_key[2];
 #pragma unroll 1
         for (int above = 0; above < 2; ++above)
-          border[above] = order_value(smallest_key([&](unsigned k) { return bin_of(k) <= bin - above; },
-                                                   (float)((ceiling + 0.5 - (double)((bin + 1 - above) << shift)) / per_t), order_key(INFINITY), lane));
+          border_key[above] = smallest_key([&](unsigned k) { return bin_of(k) <= bin - above; },
+                                           (float)((ceiling + 0.5 - (double)((bin + 1 - above) << shift)) / per_t), order_key(INFINITY), lane);
+        bin_first = border_key[0], bin_keys = border_key[1] - border_key[0];
+        border[0] = order_value(border_key[0]), border[1] = order_value(border_key[1]);
         // the next part's tokens are in flight while this part's are looked at
         constexpr int R = kPart / 64;
         auto needed = [&](int lo) {
@@ -585,27 +588,18 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
         if (ties >= all_sum(equal, sh, lane, wave)) break;  // all of them
         want = ties;
         bits = 20;
-      } else if (in_lds) {  // the highest bit in which the listed tokens differ
-        unsigned ones = 0, zeros = 0;
-        for (int i = from; i < end; i += step) ones |= sh.listed[i].x, zeros |= ~sh.listed[i].x;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) ones |= (unsigned)__shfl_xor((int)ones, o, 64), zeros |= (unsigned)__shfl_xor((int)zeros, o, 64);
-        if (lane == 0) sh.wave_u[wave] = ones, sh.wave_u[kRowWaves + wave] = zeros;
-        __syncthreads();
-        ones = zeros = 0;
-#pragma unroll
-        for (int w = 0; w < kRowWaves; ++w) ones |= sh.wave_u[w], zeros |= sh.wave_u[kRowWaves + w];
-        common = ones;
-        bits = (ones & zeros) == 0 ? 0 : 32 - __clz((int)(ones & zeros));
+      } else if (in_lds) {  // keys of the bin count from its smallest
+        common = bin_first;
+        bits = bin_keys > 1 ? 32 - __clz((int)(bin_keys - 1)) : 0;
       }
       if (phase == 0 && in_lds) want -= sh.found_above;
       if (phase == 1) {
         const double x = in_lds ? ceil(want_d - (bin ? sh.upto_weight[bin - 1] : 0.0)) : ceil(want_d / 256);
         want = x < 1.0 ? 1 : (u64)x;
       }
-      const unsigned key = find_key(
-          from, end, step, common, bits,
-          [&](int i) { return phase == 2 ? (unsigned)(kMostVocab - 1) - (in_lds ? sh.listed[i].y : (unsigned)i) : key_at(i); },
+      const unsigned key = common + find_key(
+          from, end, step, bits,
+          [&](int i) { return phase == 2 ? (unsigned)(kMostVocab - 1) - (in_lds ? sh.listed[i].y : (unsigned)i) : key_at(i) - common; },
           [&](int i) -> u64 {
             const unsigned k = key_at(i);
             return phase == 2 ? k == t_key : k == 0 ? 0 : phase == 0 ? 1 : row_weight(k) >> wide_sum;
@@ -613,6 +607,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
           want, sh, tid, lane, wave);
       if (phase == 0) {
         t_key = key, ties = want;
+        if (!(s.p < 1.f)) continue;
         // what the first k weigh: above the bin, and the listed tokens above the cut (or the row's tokens above it)
         double w = in_lds && tid == 0 && bin ? sh.upto_weight[bin - 1] : 0.0;
         for (int i = from; i < end; i += step) {
