@@ -10,8 +10,8 @@
 // Weights are exp in 64 bits rounded to fixed point, so sums by atomics are the same in any order; stretches are joined in 64-bit floating
 // point in a fixed order.  A row's result depends neither on the batch nor on scheduling.
 // What bounds it, 256 rows of 152064 logits: the first launch reads them in 25.3 us (6.2 TB/s) when it takes the maximum alone; the
-// exponential in 64 bits makes that 40.7, the bins 48.  The second takes 43, most of it for the tokens of the cut's bin: nearly every
-// stretch has some and is read again.  One row of 32000: 5.4 and 19 us, latency and a cold instruction cache.
+// exponential in 64 bits makes that 40.7, the bins 49.  The second takes 42, most of it for the tokens of the cut's bin: nearly every
+// stretch has some and is read again.  One row of 32000: 5.4 and 18 us, latency and a cold instruction cache.
 #include <mutex>
 
 #include "ctx.h"
