@@ -619,11 +619,12 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(attn_m
       }
     }
   }
-  float lw[G], acc[G][8];
+  float lw[G], acc[G][8], m0[G];
 #pragma unroll
   for (int gq = 0; gq < G; ++gq) {
 #pragma unroll
     for (int o = LPT; o < 64; o <<= 1) mw[gq] = fmaxf(mw[gq], __shfl_xor(mw[gq], o, 64));
+    m0[gq] = mw[gq] == -INFINITY ? 0.f : mw[gq];  // every score is -inf (or there is no token): every probability 0
     lw[gq] = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[gq][e] = 0.f;
@@ -638,7 +639,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(attn_m
       for (int gq = 0; gq < G; ++gq) {
         // the hardware exponential as it is: the argument is <= 0 and a result below the normal range may go to zero
         // (the library call rescales around the instruction to return subnormals)
-        const float p = ok[pp][it] ? __builtin_amdgcn_exp2f(sc[gq][pp][it] - mw[gq]) : 0.f;
+        const float p = __builtin_amdgcn_exp2f(sc[gq][pp][it] - m0[gq]);  // (-inf where there is no token)
         lw[gq] += p;
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[gq][e] += p * vv[e];

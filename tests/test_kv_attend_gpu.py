@@ -263,3 +263,71 @@ def test_rows_of_no_pages_are_refused(max_pages):
         with pytest.raises(hb.HarliError) as e:
             call()
         assert e.value.status == hb.HARLI_ERR_INVALID
+
+
+def mask_keys(case, spans):
+    """Keys of the given (sequence, first, end) become -inf in their first element: with queries positive there, scores of -inf."""
+    for b, lo, hi in spans:
+        t = np.arange(lo, hi)
+        page = case.table[b, t // P]
+        case.K[0][b][0][lo:hi, :, 0] = -np.inf
+        case.cache[page // case.ppb, 0, 0, page % case.ppb, :, t % P, 0] = float("-inf")
+    case.reset()
+
+
+@pytest.mark.parametrize("dtype,heads", [("bf16", h) for h in BF16_HEADS] + [("f32", h) for h in F32_HEADS], ids=str)
+def test_stretches_of_tokens_whose_scores_are_minus_infinity(dtype, heads):
+    """exp(-inf) is a weight of zero like any other, also where it is all that a wave (32 or 64 tokens) or a chunk has: the newest token alone
+    in its wave, whole waves, whole chunks at either end, everything but one token."""
+    case = CacheCase([65, 33, 200, 700, 700, 3000, 129, 17], *heads, dtype=dtype)
+    mask_keys(case, [(0, 64, 65), (1, 32, 33), (2, 64, 128), (3, 0, 512), (4, 256, 700), (5, 1, 3000), (6, 0, 128), (7, 0, 16)])
+    q = queries(case)
+    q[:, :, 0] = np.abs(q[:, :, 0]) + 0.25
+    out = torch.full((case.B, case.n_q, case.d), float("nan"), device=DEV)
+    before = case.got_records()
+    case.attend(torch.from_numpy(q).to(DEV), out, decay=0.5)
+    torch.cuda.synchronize()
+    case.ctx.check()
+    full = case.K[0]
+    zero = [np.isneginf(K) for K, _ in full]
+    for b in range(case.B):                                   # the oracle's weights of those tokens are zeros
+        prob = O.attend_weights(q[b], *full[b], before["w"][0, case.slots(b, int(case.n[b]))[0], :, case.slots(b, int(case.n[b]))[1]], 0.5, 0)[2]
+        assert np.all(prob[:, zero[b][:, 0, 0]] == 0) and np.allclose(prob.sum(1), 1)
+    rec = case.got_records()
+    for b in range(case.B):
+        n = int(case.n[b])
+        K, V = full[b]
+        page, slot = case.slots(b, n)
+        ref, weight, prob = O.attend_weights(q[b], K, V, before["w"][0, page, :, slot], 0.5, n - 1)
+        group = case.n_q // case.n_kv
+        K_of, V_of = np.where(zero[b], 0.0, K).repeat(group, 1), V.repeat(group, 1)
+        delta = (case.d + 4) * U * (np.abs(q[b].astype(np.float64)) * np.abs(K_of)).sum(-1).max(0) / np.sqrt(case.d)
+        rel, tiny = np.expm1(2 * delta) + (48 + -(-n // 128)) * U, 2.0 ** -126
+        assert np.all(np.abs(out[b].cpu().numpy().astype(np.float64) - ref) <= 2 * rel[:, None] * (prob.T[..., None] * np.abs(V_of)).sum(0) + n * tiny), b
+        got = rec["w"][0, page, :, slot].astype(np.float64)
+        bound = (rel[:, None] * prob).reshape(case.n_kv, group, n).sum(1).T + (group + 2) * U * np.abs(weight) + group * tiny
+        assert np.all(np.abs(got - weight) <= bound), b
+
+
+@pytest.mark.parametrize("dtype,heads", [("bf16", (4, 4, 64)), ("bf16", (8, 2, 128)), ("bf16", (7, 1, 128)), ("f32", (4, 2, 64))], ids=str)
+def test_a_value_that_is_not_a_number_reaches_its_own_element_and_a_key_its_own_head(dtype, heads):
+    case = CacheCase([100, 100, 300], *heads, dtype=dtype)
+    q = queries(case, scale=0.5)
+    where = {0: 40, 1: 70, 2: 299}
+    for b, kv, value in ((0, 1, np.nan), (1, 1, np.inf), (2, 0, np.nan)):
+        t = where[b]
+        page = case.table[b, t // P]
+        case.K[0][b][kv][t, 0, 3] = value
+        case.cache[page // case.ppb, 0, kv, page % case.ppb, 0, t % P, 3] = value
+    case.reset()
+    q_dev, out = torch.from_numpy(q).to(DEV), torch.zeros(case.B, case.n_q, case.d, device=DEV)
+    case.attend(q_dev, out, decay=0.0)
+    torch.cuda.synchronize()
+    case.ctx.check()
+    out, rec, group = out.cpu().numpy(), case.got_records(), case.n_q // case.n_kv
+    for b in range(3):
+        page, slot = case.slots(b, int(case.n[b]))
+        ref, weight, _ = O.attend_weights(q[b], *case.K[0][b], 0.0, 0.0, 0)
+        got = rec["w"][0, page, :, slot]
+        assert np.array_equal(np.isfinite(out[b]), np.isfinite(ref)) and np.array_equal(np.isposinf(out[b]), np.isposinf(ref)), b
+        assert np.array_equal(np.isnan(got), np.isnan(weight)) and np.isnan(weight[:, 0]).all() == (b == 2), b
