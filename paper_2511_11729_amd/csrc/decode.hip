@@ -947,7 +947,7 @@ __global__ void __launch_bounds__(D) k_attn_merge(const float* part, const int* 
 #pragma unroll
     for (int u = 0; u < 8; ++u)
       if (i0 + u < nch) {
-        const float f = exp2f(m[u] - Mn);
+        const float f = m[u] == -INFINITY ? 0.f : exp2f(m[u] - Mn);  // (a chunk of scores of -inf, maybe no other yet)
         L += l[u] * f;
         o += v[u] * f;
       }
