@@ -50,8 +50,15 @@ class KvBudget:
     decay: float = 1.0
 
 
+class _SentBack(tuple):
+    """The queue's (prompt, out) of a sequence that gave its pages back; `cell`: where the token is that it goes on from."""
+    cell = None
+
+
 class DecodeServer:
-    """Continuous batching over `harli_decode_step`.  Not thread-safe: one thread drives it."""
+    """Continuous batching over `harli_decode_step`.  Not thread-safe: one thread drives it.  A request is a prompt's length and a number of
+    tokens; its first step is fed token 0, every other one the sequence's own last token, whatever slot it has moved to and also
+    after it was sent back to the queue."""
 
     def __init__(self, ctx, pool, m, *, max_batch: int, max_len: int, stream, slab=None, sampling: Sampling | None = None,
                  budget: KvBudget | None = None):
@@ -80,11 +87,19 @@ class DecodeServer:
         # host allocator keeps an event on the stream the copy ran on and asks for it when the buffer is freed --
         # possibly after a restricted stream handed in by the caller has been destroyed.
         self.upload = torch.cuda.Stream()
-        self.tok = torch.zeros(max_batch, dtype=torch.int32, device=dev)
+        # Tokens on the device, by cell: a slot's of the last step and of the next one (the two swap), then those of sequences that wait
+        # in the queue to go on (at most max_batch: none are admitted past them), then the one that a new sequence begins with.
+        self.cells = torch.zeros(3 * max_batch + 1, dtype=torch.int32, device=dev)
         with torch.cuda.stream(self.upload):
-            self.tok.zero_()                   # first use now, not in the middle of a run
+            self.cells.zero_()                 # first use now, not in the middle of a run
         self.upload.synchronize()
-        self.nxt = torch.zeros(max_batch, dtype=torch.int32, device=dev)
+        self.tok, self.nxt = self.cells[:max_batch], self.cells[max_batch: 2 * max_batch]
+        self.tok_at, self.first_token = 0, 3 * max_batch
+        self.waiting_cells = list(range(2 * max_batch, 3 * max_batch))
+        # where each slot's token comes from, when not from the slot itself
+        self.source_ring = [torch.empty(max_batch, dtype=torch.int32, pin_memory=True) for _ in self.ring]
+        self.source_dev = torch.zeros(max_batch, dtype=torch.int32, device=dev)
+        self.fed = torch.zeros(max_batch, dtype=torch.int32, device=dev)
         self.logits = torch.empty(max_batch, m.vocab, dtype=torch.float32, device=dev)
         self.x_out = torch.empty(max_batch, m.hidden, dtype=torch.float32, device=dev)
         self.sampling, self.budget = sampling, budget
@@ -108,10 +123,10 @@ class DecodeServer:
             self.marks = np.zeros((5, max_batch), np.int32)
             self.marks_ring = [torch.empty(5, max_batch, dtype=torch.int32, pin_memory=True) for _ in self.ring]
             self.marks_dev = torch.zeros(5, max_batch, dtype=torch.int32, device=dev)
-        if sampling is not None or budget is not None:
-            torch.cuda.current_stream().synchronize()   # the buffers are filled before another stream reads them
+        torch.cuda.current_stream().synchronize()   # the buffers are filled before another stream reads them
         self.evicted = 0           # tokens (of every layer and KV head alike) that have left the cache under a budget
-        self.running = []          # per slot: [pages (list), cached tokens, tokens left, tokens it has had, just arrived, cut after this step]
+        # per slot: [pages (list), cached tokens, tokens left, tokens it has had, just arrived, cut after this step, cell of its next token]
+        self.running = []
         self.queue = collections.deque()
         self.step_no = 0
         self.last_done = None
@@ -152,7 +167,7 @@ class DecodeServer:
                     raise
                 self.kv_stalls += 1            # no room for this prompt now: it stays queued
                 break
-            self.queue.popleft()
+            cell = getattr(self.queue.popleft(), "cell", None)
             if self.kv_view is not None:       # the prompt's cache "arrives": its pages are written once
                 # One fill per run of neighbouring pages, on the decode stream, and no index tensor: copying one to the
                 # device would make the host wait for every step it has queued, and anything on the default stream
@@ -171,7 +186,7 @@ class DecodeServer:
             self.table[b, :] = -1
             self.table[b, :need] = ids
             self.kv[b] = prompt
-            self.running.append([list(ids), prompt, out, prompt, True, False])
+            self.running.append([list(ids), prompt, out, prompt, True, False, self.first_token if cell is None else cell])
             self.admitted += 1
 
     def _drop(self, b, event):
@@ -199,6 +214,11 @@ class DecodeServer:
             ev.synchronize()                   # the copy that last used this staging buffer is done
         tb[:B].copy_(torch.from_numpy(self.table[:B]))
         kb[:B].copy_(torch.from_numpy(self.kv[:B]))
+        source = [seq[6] for seq in self.running]
+        moved = source != list(range(self.tok_at, self.tok_at + B))
+        if moved:
+            staged = self.source_ring[self.step_no % len(self.ring)]
+            staged[:B].copy_(torch.tensor(source, dtype=torch.int32))
         if self.budget is not None:
             for b, seq in enumerate(self.running):
                 after = seq[1] + 1
@@ -211,6 +231,8 @@ class DecodeServer:
         with torch.cuda.stream(self.upload):
             self.table_dev[:B].copy_(tb[:B], non_blocking=True)
             self.kv_dev[:B].copy_(kb[:B], non_blocking=True)
+            if moved:
+                self.source_dev[:B].copy_(staged[:B], non_blocking=True)
             if self.budget is not None:
                 self.marks_dev.copy_(marks, non_blocking=True)
             up = torch.cuda.Event()
@@ -218,7 +240,11 @@ class DecodeServer:
         self.stream.wait_event(up)
         start = torch.cuda.Event(enable_timing=True)
         start.record(self.stream)
-        self._launch(B, int(self.kv[:B].max()) + 1)
+        self._keep_waiting_tokens()
+        if moved:
+            with torch.cuda.stream(self.stream):
+                torch.index_select(self.cells, 0, self.source_dev[:B], out=self.fed[:B])
+        self._launch(B, int(self.kv[:B].max()) + 1, self.fed if moved else self.tok)
         done = torch.cuda.Event(enable_timing=True)
         done.record(self.stream)
         self._timed.append((start if self.last_done is None or self._idle else self.last_done, done, self.tag))
@@ -226,6 +252,11 @@ class DecodeServer:
         self.last_done = done
         self.ring[self.step_no % len(self.ring)] = (tb, kb, up)
         self.tok, self.nxt = self.nxt, self.tok   # the tokens just produced feed the next step
+        self.tok_at = self.max_batch - self.tok_at
+        for b, seq in enumerate(self.running):
+            if 2 * self.max_batch <= seq[6] < self.first_token:
+                self.waiting_cells.append(seq[6])
+            seq[6] = self.tok_at + b
         self.step_no += 1
         self.tokens_out += B
         if len(self._held) > 256 and self.pool.stats().pending_frees == 0:
@@ -263,16 +294,29 @@ class DecodeServer:
                         raise
                     # the reserve is there to prevent this; if it happens the sequence goes back to the queue
                     self.preempted += 1
-                    self.queue.appendleft((seq[3], seq[2]))   # (as a prompt of all tokens it has had, those that left its cache too)
+                    back = _SentBack((seq[3], seq[2]))   # (as a prompt of all tokens it has had, those that left its cache too)
+                    back.cell = seq[6]
+                    self.queue.appendleft(back)
                     self._drop(b, done)
                     continue
             b += 1
         return done, B, start
 
-    def _launch(self, B, max_kv):
+    def _keep_waiting_tokens(self):
+        """Tokens of sequences that were sent back and wait on move out of the cells that this step's slots write, on the decode stream."""
+        for entry in self.queue:
+            if not isinstance(entry, _SentBack):
+                break                           # (they are the first in the queue)
+            if entry.cell < 2 * self.max_batch:
+                cell = self.waiting_cells.pop()
+                with torch.cuda.stream(self.stream):
+                    self.cells[cell: cell + 1].copy_(self.cells[entry.cell: entry.cell + 1])
+                entry.cell = cell
+
+    def _launch(self, B, max_kv, tokens):
         """The step's calls, in order on the decode stream."""
         step = dict(batch=B, kv_len=self.kv_dev, page_table=self.table_dev, max_pages=self.max_pages, max_kv_len=max_kv,
-                    token_ids=self.tok, x_out=self.x_out, logits=self.logits, next_token=None if self.sampling else self.nxt,
+                    token_ids=tokens, x_out=self.x_out, logits=self.logits, next_token=None if self.sampling else self.nxt,
                     stream=self.stream)
         if self.budget is None:
             self.ctx.decode_step(**step)
