@@ -58,7 +58,8 @@ class _SentBack(tuple):
 class DecodeServer:
     """Continuous batching over `harli_decode_step`.  Not thread-safe: one thread drives it.  A request is a prompt's length and a number of
     tokens; its first step is fed token 0, every other one the sequence's own last token, whatever slot it has moved to and also
-    after it was sent back to the queue."""
+    after it was sent back to the queue.  A prompt arrives whole, inside a budget too, and so does a sequence that was sent back: one of
+    more tokens than the pool has room for is dropped and counted in `refused`."""
 
     def __init__(self, ctx, pool, m, *, max_batch: int, max_len: int, stream, slab=None, sampling: Sampling | None = None,
                  budget: KvBudget | None = None):
@@ -131,6 +132,7 @@ class DecodeServer:
         self.step_no = 0
         self.last_done = None
         self.admitted = self.finished = self.kv_stalls = self.preempted = self.tokens_out = 0
+        self.refused = 0           # requests, also ones sent back, that the whole pool could not hold: they leave the queue
         self._held = []            # events handed to the pool with freed pages: alive until the pool has polled them
         self.tag = None            # whatever the caller wants kept with the next step (see completed_steps)
         self._timed = collections.deque()
@@ -152,10 +154,16 @@ class DecodeServer:
             prompt = min(prompt, self.max_len - 2)
             out = max(1, min(out, self.max_len - 1 - prompt))
             need = (prompt + 1 + P - 1) // P
+            st = self.pool.stats()
+            if need > st.n_chunks * st.pages_per_block:   # not even an empty pool could take it: it must not hold up those behind it
+                cell = getattr(self.queue.popleft(), "cell", None)
+                if cell is not None and cell >= 2 * self.max_batch:
+                    self.waiting_cells.append(cell)
+                self.refused += 1
+                continue
             # headroom: besides the prompt, one more page for every sequence that is running (each reaches a page
             # boundary within 16 steps); without it a pool smaller than the KV demand admits, runs out, sends a
             # sequence back to the queue and admits it again, over and over
-            st = self.pool.stats()
             free_pages = (st.kv_chunks + st.free_chunks) * st.pages_per_block - st.kv_pages_live
             if self.running and need + len(self.running) > free_pages:
                 self.kv_stalls += 1
@@ -483,7 +491,7 @@ def replay(server: DecodeServer, arrivals, worker_factory=None, slo_ms=40.0, sam
            "tpot_ms_p99": float(np.percentile(tpot, 99)), "tpot_ms_max": float(tpot.max()), "within_slo": float(np.mean(tpot <= slo_ms)),
            "batch_mean": float(batches.mean()) if len(batches) else 0.0, "batch_max": int(batches.max()) if len(batches) else 0,
            "admitted": server.admitted, "finished": server.finished, "kv_admission_stalls": server.kv_stalls,
-           "preempted": server.preempted, "queued_at_end": len(server.queue), "tokens_evicted": server.evicted, "snapshots": snaps,
+           "preempted": server.preempted, "refused": server.refused, "queued_at_end": len(server.queue), "tokens_evicted": server.evicted, "snapshots": snaps,
            "plans": plans if plan is not None else [], "tpot_ms": tpot, "batches": batches, "step_ms": busy}
     if ft is not None:
         ft["tokens_per_s"] = ft["tokens"] / elapsed

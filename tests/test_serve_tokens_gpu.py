@@ -116,3 +116,37 @@ def test_a_sequence_that_was_sent_back_goes_on_from_its_own_token(budget):
     assert server.preempted >= 3 and server.finished == 4
     for prompt, out in requests:
         assert fed(ctx.log, prompt + out, prompt) == chain(prompt, out), (prompt, out)
+
+
+def test_a_prompt_that_the_pool_can_never_hold_does_not_hold_up_the_others():
+    server, ctx, pool = service(1)                                 # 16 pages: 256 tokens
+    server.submit([(10, 3), (256, 4), (255, 1), (1000, 5), (20, 6)])
+    for _ in range(40):
+        server.step()
+        server.stream.synchronize()                                # (what was freed can be had again)
+    assert not server.queue and not server.running
+    assert server.finished == 3 and server.refused == 2 and server.admitted == 3
+    assert pool.stats().kv_pages_live == 0 or pool.stats().pending_frees > 0
+
+
+@pytest.mark.parametrize("budget", [None, serve.KvBudget(keep=48, slack=32, sink=2, recent=12)], ids=["whole", "budget"])
+def test_a_sequence_that_outgrew_the_pool_and_was_sent_back_does_not_hold_up_the_others(budget):
+    server, ctx, pool = service(1, max_batch=2, budget=budget)
+    server.submit([(60, 900)])
+    for _ in range(200):                                           # 256 tokens and more, inside a budget in at most six pages
+        server.step()
+    alloc = pool.alloc_pages
+
+    def none_left(n):
+        raise hb.HarliError(hb.HARLI_ERR_OOM, "none left")
+    pool.alloc_pages = none_left
+    for _ in range(40):
+        server.step()
+    pool.alloc_pages = alloc
+    assert server.preempted == 1 and not server.running
+    assert server.refused == 1 and not server.queue                # its history is longer than 256 tokens
+    server.submit([(20, 6), (30, 4)])
+    for _ in range(20):
+        server.step()
+        server.stream.synchronize()
+    assert server.finished == 2
