@@ -319,7 +319,7 @@ def main():
         keep[-1].zero_()                             # first use of the stream now (its hardware queue is set up here)
     sD.synchronize()
     sampling = None if args.temperature is None else serve.Sampling(args.temperature, args.top_k, args.top_p, args.min_p)
-    budget = None if args.kv_budget is None else serve.KvBudget(args.kv_budget)
+    budget = None if args.kv_budget is None else serve.KvBudget.of(args.kv_budget)
     server = serve.DecodeServer(ctx, pool, m, max_batch=args.max_batch, max_len=args.max_len, stream=sD, slab=keep[0], sampling=sampling,
                                 budget=budget)
     arrivals = wl.make_arrivals(w, args.steps, tuple(args.targets), args.mean_out,

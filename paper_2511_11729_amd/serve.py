@@ -42,12 +42,20 @@ class Sampling:
 @dataclasses.dataclass(frozen=True)
 class KvBudget:
     """A sequence that holds `keep` + `slack` tokens is cut to `keep` (harli_kv_evict): the first `sink` and the last `recent`
-    positions stay, of the others those with the most accumulated attention weight."""
+    positions stay, of the others those with the most accumulated attention weight.  `keep` has room for sink + recent."""
     keep: int
     slack: int = P
     sink: int = 4
     recent: int = 64
     decay: float = 1.0
+
+    @classmethod
+    def of(cls, keep: int, **kw) -> KvBudget:
+        """A budget of `keep` tokens; where that has no room for the usual sink and recent positions, half of it is for the newest ones and
+        up to a quarter for the first."""
+        if keep < cls.sink + cls.recent:
+            kw = dict(dict(sink=min(cls.sink, keep // 4), recent=max(1, keep // 2)), **kw)
+        return cls(keep, **kw)
 
 
 class _SentBack(tuple):
@@ -116,6 +124,10 @@ class DecodeServer:
                 raise ValueError("a budget keeps at least one token and cuts at least one")
             if max_len > 1 << 18:
                 raise ValueError("a budget is for sequences of at most 2^18 tokens (harli_kv_evict)")
+            if budget.sink < 0 or budget.recent < 0 or not 0 <= budget.decay <= 1:
+                raise ValueError("a budget's sink and recent are not negative, and its decay is 0..1")
+            if budget.sink + budget.recent > budget.keep:   # the newest tokens would leave: among protected ones the lower slot stays
+                raise ValueError("a budget of %d tokens cannot keep %d first and %d last ones" % (budget.keep, budget.sink, budget.recent))
             st = pool.stats()
             self.track = torch.zeros(pool.cfg.n_layers, st.n_chunks * st.pages_per_block, m.n_kv, P, 2, dtype=torch.int32, device=dev)
             self.attend_ws = torch.empty(ctx.kv_attend_workspace_bytes(max_batch, max_len), dtype=torch.uint8, device=dev)

@@ -150,3 +150,20 @@ def test_a_sequence_that_outgrew_the_pool_and_was_sent_back_does_not_hold_up_the
         server.step()
         server.stream.synchronize()
     assert server.finished == 2
+
+
+@pytest.mark.parametrize("budget", [dict(keep=32), dict(keep=67), dict(keep=20, sink=4, recent=17), dict(keep=64, sink=0, recent=65),
+                                    dict(keep=80, sink=-1), dict(keep=80, recent=-1), dict(keep=80, decay=1.5), dict(keep=80, decay=-0.1),
+                                    dict(keep=80, decay=float("nan"))], ids=str)
+def test_budgets_that_cannot_keep_what_they_promise_are_refused(budget):
+    with pytest.raises(ValueError):
+        service(1, budget=serve.KvBudget(**budget))
+
+
+@pytest.mark.parametrize("keep", [1, 2, 5, 8, 32, 67, 68, 69, 512])
+def test_the_protection_of_a_small_budget_fits_it(keep):
+    budget = serve.KvBudget.of(keep)
+    assert budget.keep == keep and 1 <= budget.recent <= 64 and 0 <= budget.sink <= 4 and budget.sink + budget.recent <= keep
+    service(1, budget=budget)
+    if keep >= 68:
+        assert budget == serve.KvBudget(keep)
