@@ -303,6 +303,8 @@ def main():
                     help="cached tokens per sequence: past it the least attended ones leave, a page's worth at a time")
     ap.add_argument("--sched-margin", type=float, default=0.9, help="the scheduler plans for this fraction of the target")
     args = ap.parse_args()
+    if args.temperature is None and (args.top_k or args.top_p != 1.0 or args.min_p):
+        ap.error("--top-k, --top-p and --min-p are for drawn tokens: give --temperature")
 
     import faulthandler
     import torch

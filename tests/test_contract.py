@@ -34,3 +34,9 @@ def test_product_package_and_benchmark_paths_do_not_import_the_oracle():
     src = open(os.path.join(ROOT, "bench.py")).read()
     hits = [m.start() for m in pat.finditer(src)]
     assert len(hits) == 1 and "no_cpu_baseline" in src[max(0, hits[0] - 400): hits[0]]
+
+
+def test_bench_serve_refuses_filters_of_tokens_that_are_not_drawn():
+    for flag in (["--top-k", "40"], ["--top-p", "0.9"], ["--min-p", "0.1"]):
+        r = subprocess.run([sys.executable, "-m", "paper_2511_11729_amd.bench_serve"] + flag, capture_output=True, text=True, cwd=ROOT, timeout=120)
+        assert r.returncode == 2 and "--temperature" in r.stderr and r.stdout.strip() == ""
