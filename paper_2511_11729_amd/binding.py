@@ -27,6 +27,13 @@ class HarliError(RuntimeError):
         self.status = status
 
 
+class HarliArgumentError(HarliError, ValueError):
+    """An argument that the binding refuses before the library sees its address."""
+
+    def __init__(self, msg: str):
+        super().__init__(HARLI_ERR_INVALID, msg)
+
+
 class PoolCfg(C.Structure):
     _fields_ = [("block_bytes", C.c_size_t), ("n_layers", C.c_int32), ("page_tokens", C.c_int32),
                 ("kv_row_bytes", C.c_size_t), ("small_pool_bytes", C.c_size_t), ("small_granule", C.c_size_t),
@@ -220,6 +227,37 @@ def _ptr(t) -> Optional[int]:
     if isinstance(t, int):
         return t
     return t.data_ptr()
+
+
+def _array(who: str, name: str, t, kind: str, least: int) -> None:
+    """Refuses a tensor that is not `least` or more values of `kind` ("float32", "int32"; "word": either) side by side: the library would
+    read a wrong type's halves, or past the end.  None and raw addresses pass."""
+    if t is None or t.__class__ is int:
+        return
+    types = _TYPES or _types()
+    if t.dtype not in types[kind] or t.numel() < least or not t.is_contiguous():
+        raise HarliArgumentError("%s: %s has to be %d or more contiguous values of %s, not %s of %s with steps %s" % (
+            who, name, least, kind if kind != "word" else "four bytes", tuple(t.shape), t.dtype, t.stride()))
+
+
+_TYPES = {}
+
+
+def _types() -> dict:
+    import torch
+    _TYPES.update(float32=(torch.float32,), int32=(torch.int32,), word=(torch.int32, torch.float32))
+    return _TYPES
+
+
+def _on_device(who: str, *arrays) -> None:
+    """Refuses tensors that are not all on one device."""
+    at = None
+    for t in arrays:
+        if t is None or t.__class__ is int:
+            continue
+        if not t.is_cuda or at not in (None, t.get_device()):
+            raise HarliArgumentError("%s: arrays have to be on one device" % who)
+        at = t.get_device()
 
 
 def _stream(s) -> Optional[int]:
@@ -478,11 +516,24 @@ def adamw_step(master, m, v, grad, param_bf16, *, step: int, lr=1e-3, beta1=0.9,
 
 def sample(logits, uniform, token, *, workspace, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, stream=None) -> None:
     """A token per row of logits (fp32 [batch, vocab], rows may lie apart) from the random numbers `uniform`; the settings are device
-    tensors [batch] or None.  workspace: sample_workspace_bytes(batch, vocab) bytes on the device."""
+    tensors [batch] or None.  token and top_k are int32, uniform, logprob and the other settings fp32; longer ones may be given.
+    workspace: sample_workspace_bytes(batch, vocab) bytes on the device."""
     if logits.dim() != 2 or str(logits.dtype) != "torch.float32" or (logits.shape[1] > 1 and logits.stride(1) != 1):
-        raise ValueError("sample: logits have to be fp32 [batch, vocab], a row's side by side")
-    b = SampleBatch(logits.shape[0], logits.shape[1], _ptr(logits), logits.stride(0), _ptr(uniform), _ptr(temperature), _ptr(top_k),
-                    _ptr(top_p), _ptr(min_p), _ptr(token), _ptr(logprob), _ptr(workspace), workspace.numel() * workspace.element_size())
+        raise HarliArgumentError("sample: logits have to be fp32 [batch, vocab], a row's side by side")
+    n, vocab = logits.shape
+    _array("sample", "uniform", uniform, "float32", n)
+    _array("sample", "token", token, "int32", n)
+    _array("sample", "temperature", temperature, "float32", n)
+    _array("sample", "top_k", top_k, "int32", n)
+    _array("sample", "top_p", top_p, "float32", n)
+    _array("sample", "min_p", min_p, "float32", n)
+    _array("sample", "logprob", logprob, "float32", n)
+    _on_device("sample", logits, uniform, token, temperature, top_k, top_p, min_p, logprob, workspace)
+    if not workspace.is_contiguous():
+        raise HarliArgumentError("sample: workspace has to be contiguous")
+    ld = logits.stride(0) if n > 1 else max(vocab, logits.stride(0))   # (one row: its step means nothing)
+    b = SampleBatch(n, vocab, _ptr(logits), ld, _ptr(uniform), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(token),
+                    _ptr(logprob), _ptr(workspace), workspace.numel() * workspace.element_size())
     _check(lib().harli_sample(C.byref(b), _stream(stream)))
 
 
