@@ -1,12 +1,14 @@
 """ctypes binding of libharli.so: same names as include/harli.h, argument marshalling only.
 
 Every step of the path runs inside the HIP library; this module converts Python
-values to C structs and raises on a non-zero status.  It fails loudly if the
-library has not been built (`python -m paper_2511_11729_amd.build`).
+values to C structs and raises on a non-zero status.  The calls of a budgeted cache
+and `sample` also refuse tensors of a type, length or place that the library would
+misread.  It fails loudly if the library has not been built (`python -m paper_2511_11729_amd.build`).
 """
 from __future__ import annotations
 
 import ctypes as C
+import struct
 import sys
 import os
 from typing import List, Optional, Sequence
@@ -115,6 +117,19 @@ class SampleBatch(C.Structure):
                 ("token", C.c_void_p), ("logprob", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
+def _packer(cls):
+    """A function from the values of a struct's fields, those of a struct in it among them, to its bytes (a fifth of the time that making
+    the struct takes: the calls of a decode step are as short as their launches)."""
+    code = {C.c_int32: "i", C.c_void_p: "P", C.c_float: "f", C.c_size_t: "N", C.c_int64: "q"}
+    fields = lambda c: "".join(code[t] if t in code else fields(t) for _, t in c._fields_)  # noqa: E731
+    s = struct.Struct("@" + fields(cls) + "0P")
+    assert s.size == C.sizeof(cls)
+    return s.pack
+
+
+_pack_decode, _pack_tracking, _pack_attend, _pack_record, _pack_evict, _pack_sample = map(
+    _packer, (DecodeBatch, Tracking, AttendBatch, RecordBatch, EvictBatch, SampleBatch))
+
 _lib = None
 
 _SIGS = {
@@ -137,12 +152,12 @@ _SIGS = {
     "harli_decode_step": (C.c_int, [C.c_void_p, C.POINTER(DecodeBatch), C.c_void_p]),
     "harli_decode_step_static": (C.c_int, [C.c_void_p, C.POINTER(DecodeBatch), C.c_void_p]),
     "harli_decode_step_static_bytes": (C.c_size_t, [C.c_void_p, C.c_int32, C.c_int32]),
-    "harli_decode_step_tracked": (C.c_int, [C.c_void_p, C.POINTER(DecodeBatch), C.POINTER(Tracking), C.c_void_p]),
-    "harli_kv_attend": (C.c_int, [C.c_void_p, C.POINTER(AttendBatch), C.c_void_p]),
+    "harli_decode_step_tracked": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "harli_kv_attend": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]),
     "harli_kv_attend_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_int32, C.c_int32]),
-    "harli_kv_record_init": (C.c_int, [C.c_void_p, C.POINTER(RecordBatch), C.c_void_p]),
-    "harli_kv_evict": (C.c_int, [C.c_void_p, C.POINTER(EvictBatch), C.c_void_p]),
-    "harli_sample": (C.c_int, [C.POINTER(SampleBatch), C.c_void_p]),
+    "harli_kv_record_init": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]),
+    "harli_kv_evict": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]),
+    "harli_sample": (C.c_int, [C.c_void_p, C.c_void_p]),
     "harli_sample_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32]),
     "harli_lora_fwd": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
                                  C.POINTER(C.c_void_p), C.c_void_p]),
@@ -229,35 +244,37 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
-def _array(who: str, name: str, t, kind: str, least: int) -> None:
-    """Refuses a tensor that is not `least` or more values of `kind` ("float32", "int32"; "word": either) side by side: the library would
-    read a wrong type's halves, or past the end.  None and raw addresses pass."""
-    if t is None or t.__class__ is int:
-        return
-    types = _TYPES or _types()
-    if t.dtype not in types[kind] or t.numel() < least or not t.is_contiguous():
-        raise HarliArgumentError("%s: %s has to be %d or more contiguous values of %s, not %s of %s with steps %s" % (
-            who, name, least, kind if kind != "word" else "four bytes", tuple(t.shape), t.dtype, t.stride()))
+_INT = _FLOAT = None   # torch's types of int32 and fp32 tensors on a device, once a call has brought a tensor
 
 
-_TYPES = {}
-
-
-def _types() -> dict:
+def _kinds() -> None:
+    global _INT, _FLOAT
     import torch
-    _TYPES.update(float32=(torch.float32,), int32=(torch.int32,), word=(torch.int32, torch.float32))
-    return _TYPES
+    _INT, _FLOAT = torch.cuda.IntTensor, torch.cuda.FloatTensor
 
 
-def _on_device(who: str, *arrays) -> None:
-    """Refuses tensors that are not all on one device."""
-    at = None
-    for t in arrays:
-        if t is None or t.__class__ is int:
-            continue
-        if not t.is_cuda or at not in (None, t.get_device()):
-            raise HarliArgumentError("%s: arrays have to be on one device" % who)
-        at = t.get_device()
+def _array(who: str, name: str, t, kind, least: int) -> int:
+    """Address of a device tensor of the type `kind` with `least` or more bytes side by side; any other is refused: the library would read a
+    wrong type's halves, past the end, or the host's memory.  None is 0, and raw addresses pass."""
+    if isinstance(t, kind) and t.nbytes >= least and t.is_contiguous():
+        return t.data_ptr()
+    if t is None:
+        return 0
+    if isinstance(t, int):
+        return t
+    if name == "track" and kind is _INT:             # records are words of either type
+        return _array(who, name, t, _FLOAT, least)
+    raise HarliArgumentError("%s: %s has to be %d or more contiguous values of %s on the device, not %s of %s on %s with steps %s" % (
+        who, name, least // 4, "int32" if kind is _INT else "fp32", tuple(t.shape), t.dtype, t.device, t.stride()))
+
+
+def _workspace(who: str, t):
+    """(address, bytes)"""
+    if t is None:
+        return 0, 0
+    if not t.is_contiguous() or not t.is_cuda:
+        raise HarliArgumentError("%s: workspace has to be contiguous, on the device" % who)
+    return t.data_ptr(), t.nbytes
 
 
 def _stream(s) -> Optional[int]:
@@ -364,6 +381,9 @@ class Context:
             for n in ("bq", "bk", "bv"):                      # optional frozen biases (fp32)
                 setattr(arr[i], n, _ptr(lw.get(n)))
         w = Weights(arr, _ptr(emb), _ptr(g_final), _ptr(w_lm))
+        st = pool.stats()
+        self.record_bytes = 8 * n_layers * st.n_chunks * st.pages_per_block * n_kv_heads * pool.cfg.page_tokens
+        self.row_values = n_q_heads * head_dim
         self.handle = C.c_void_p()
         _check(lib().harli_ctx_create(C.byref(self.cfg), C.byref(w), pool.handle, C.byref(self.handle)))
 
@@ -442,40 +462,63 @@ class Context:
     def decode_step_static_bytes(self, batch: int, max_kv_len: int) -> int:
         return int(lib().harli_decode_step_static_bytes(self.handle, batch, max_kv_len))
 
-    # ---- a cache inside a budget (harli_kv_*).  track: device records [n_layers, page ids, n_kv_heads, page_tokens, 2], four bytes each:
-    # the weight as fp32 bits, the position as int32
+    # ---- a cache inside a budget (harli_kv_*).  track: device records [n_layers, page ids, n_kv_heads, page_tokens, 2] in int32 or fp32, the
+    # weight as the bits of an fp32, the position as those of an int32.  Lengths, positions and the page table are int32, q and out fp32;
+    # longer arrays may be given.
     def decode_step_tracked(self, *, batch, kv_len, page_table, max_pages, max_kv_len, track, workspace, decay=1.0, position=None,
                             token_ids=None, x_in=None, x_out=None, logits=None, next_token=None, stream=None) -> None:
-        b = DecodeBatch(batch, _ptr(token_ids), _ptr(x_in), _ptr(x_out), _ptr(logits), _ptr(next_token), _ptr(kv_len),
-                        _ptr(page_table), max_pages, max_kv_len)
-        t = self._tracking(track, decay, position, workspace)
-        _check(lib().harli_decode_step_tracked(self.handle, C.byref(b), C.byref(t), _stream(stream)))
+        who = "decode_step_tracked"
+        if _INT is None:
+            _kinds()
+        b = _pack_decode(batch, *[_ptr(t) or 0 for t in (token_ids, x_in, x_out, logits, next_token)], _array(who, "kv_len", kv_len, _INT, 4 * batch),
+                         _array(who, "page_table", page_table, _INT, 4 * batch * max_pages), max_pages, max_kv_len)
+        t = _pack_tracking(_array(who, "track", track, _INT, self.record_bytes), decay, _array(who, "position", position, _INT, 4 * batch),
+                           *_workspace(who, workspace))
+        status = _lib.harli_decode_step_tracked(self.handle, b, t, None if stream is None else _stream(stream))
+        if status:
+            _check(status)
 
     def kv_attend(self, *, layer, batch, q, out, n_tokens, page_table, max_pages, max_kv_len, workspace, track=None, decay=1.0,
                   position=None, stream=None) -> None:
         """Attention of one new token per sequence over one layer's cache; with `track`, the weight of every cached token."""
-        b = AttendBatch(batch, layer, _ptr(q), _ptr(out), _ptr(n_tokens), _ptr(page_table), max_pages, max_kv_len,
-                        self._tracking(track, decay, position, workspace))
-        _check(lib().harli_kv_attend(self.handle, C.byref(b), _stream(stream)))
+        who, rows = "kv_attend", 4 * batch * self.row_values
+        if _INT is None:
+            _kinds()
+        b = _pack_attend(batch, layer, _array(who, "q", q, _FLOAT, rows), _array(who, "out", out, _FLOAT, rows),
+                         _array(who, "n_tokens", n_tokens, _INT, 4 * batch), _array(who, "page_table", page_table, _INT, 4 * batch * max_pages),
+                         max_pages, max_kv_len, _array(who, "track", track, _INT, self.record_bytes), decay,
+                         _array(who, "position", position, _INT, 4 * batch), *_workspace(who, workspace))
+        status = _lib.harli_kv_attend(self.handle, b, None if stream is None else _stream(stream))
+        if status:
+            _check(status)
 
     def kv_attend_workspace_bytes(self, batch: int, max_kv_len: int) -> int:
         return int(lib().harli_kv_attend_workspace_bytes(self.handle, batch, max_kv_len))
 
     def kv_record_init(self, *, batch, n_tokens, page_table, max_pages, max_kv_len, track, stream=None) -> None:
         """Records of a prompt's tokens: weight 0, position their index."""
-        b = RecordBatch(batch, _ptr(n_tokens), _ptr(page_table), max_pages, max_kv_len, _ptr(track))
-        _check(lib().harli_kv_record_init(self.handle, C.byref(b), _stream(stream)))
+        who = "kv_record_init"
+        if _INT is None:
+            _kinds()
+        b = _pack_record(batch, _array(who, "n_tokens", n_tokens, _INT, 4 * batch), _array(who, "page_table", page_table, _INT, 4 * batch * max_pages),
+                         max_pages, max_kv_len, _array(who, "track", track, _INT, self.record_bytes))
+        status = _lib.harli_kv_record_init(self.handle, b, None if stream is None else _stream(stream))
+        if status:
+            _check(status)
 
     def kv_evict(self, *, batch, n_tokens, keep, page_table, max_pages, max_kv_len, track, sink=0, recent=0, position=None, n_left=None,
                  stream=None) -> None:
         """Every layer and KV head of sequence b keeps its best keep[b] tokens, in its first keep[b] slots."""
-        b = EvictBatch(batch, _ptr(n_tokens), _ptr(keep), _ptr(position), _ptr(page_table), max_pages, max_kv_len, sink, recent,
-                       _ptr(track), _ptr(n_left))
-        _check(lib().harli_kv_evict(self.handle, C.byref(b), _stream(stream)))
-
-    @staticmethod
-    def _tracking(track, decay, position, workspace) -> Tracking:
-        return Tracking(_ptr(track), decay, _ptr(position), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
+        who, each = "kv_evict", 4 * batch
+        if _INT is None:
+            _kinds()
+        b = _pack_evict(batch, _array(who, "n_tokens", n_tokens, _INT, each), _array(who, "keep", keep, _INT, each),
+                        _array(who, "position", position, _INT, each), _array(who, "page_table", page_table, _INT, each * max_pages),
+                        max_pages, max_kv_len, sink, recent, _array(who, "track", track, _INT, self.record_bytes),
+                        _array(who, "n_left", n_left, _INT, each))
+        status = _lib.harli_kv_evict(self.handle, b, None if stream is None else _stream(stream))
+        if status:
+            _check(status)
 
     def lora_fwd(self, layer: int, X, Y, B_f: int, S: int, stream=None) -> int:
         saved = C.c_void_p()
@@ -518,23 +561,17 @@ def sample(logits, uniform, token, *, workspace, temperature=None, top_k=None, t
     """A token per row of logits (fp32 [batch, vocab], rows may lie apart) from the random numbers `uniform`; the settings are device
     tensors [batch] or None.  token and top_k are int32, uniform, logprob and the other settings fp32; longer ones may be given.
     workspace: sample_workspace_bytes(batch, vocab) bytes on the device."""
-    if logits.dim() != 2 or str(logits.dtype) != "torch.float32" or (logits.shape[1] > 1 and logits.stride(1) != 1):
-        raise HarliArgumentError("sample: logits have to be fp32 [batch, vocab], a row's side by side")
+    if _INT is None:
+        _kinds()
+    if logits.dim() != 2 or not isinstance(logits, _FLOAT) or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise HarliArgumentError("sample: logits have to be fp32 [batch, vocab] on the device, a row's side by side")
     n, vocab = logits.shape
-    _array("sample", "uniform", uniform, "float32", n)
-    _array("sample", "token", token, "int32", n)
-    _array("sample", "temperature", temperature, "float32", n)
-    _array("sample", "top_k", top_k, "int32", n)
-    _array("sample", "top_p", top_p, "float32", n)
-    _array("sample", "min_p", min_p, "float32", n)
-    _array("sample", "logprob", logprob, "float32", n)
-    _on_device("sample", logits, uniform, token, temperature, top_k, top_p, min_p, logprob, workspace)
-    if not workspace.is_contiguous():
-        raise HarliArgumentError("sample: workspace has to be contiguous")
-    ld = logits.stride(0) if n > 1 else max(vocab, logits.stride(0))   # (one row: its step means nothing)
-    b = SampleBatch(n, vocab, _ptr(logits), ld, _ptr(uniform), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(token),
-                    _ptr(logprob), _ptr(workspace), workspace.numel() * workspace.element_size())
-    _check(lib().harli_sample(C.byref(b), _stream(stream)))
+    b = _pack_sample(n, vocab, logits.data_ptr(), logits.stride(0) if n > 1 else max(vocab, logits.stride(0)),   # (one row: its step means nothing)
+                     _array("sample", "uniform", uniform, _FLOAT, 4 * n), _array("sample", "temperature", temperature, _FLOAT, 4 * n),
+                     _array("sample", "top_k", top_k, _INT, 4 * n), _array("sample", "top_p", top_p, _FLOAT, 4 * n),
+                     _array("sample", "min_p", min_p, _FLOAT, 4 * n), _array("sample", "token", token, _INT, 4 * n),
+                     _array("sample", "logprob", logprob, _FLOAT, 4 * n), *_workspace("sample", workspace))
+    _check(lib().harli_sample(b, _stream(stream)))
 
 
 def sample_workspace_bytes(batch: int, vocab: int) -> int:
