@@ -424,6 +424,10 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
         if (usable(logit(i))) whole_mine += (double)row_weight(order_key(logit(i)));
     }
     double among = all_sum(whole_mine, sh, lane, wave);  // weight of the tokens that top-k leaves, in the row's fixed point
+    // Bits that a search of the whole row drops from every weight, so that the sum of all fits 63: none up to 2^13 times the largest weight,
+    // 8 at most.  All tokens together lose less than 2^-42 of their sum by it (with 8 dropped from every row's, a tail of light tokens
+    // behind a heavy one lost a part of itself, and top-p near 1 kept too many of it).
+    const int wide = max(0, __builtin_amdgcn_frexp_exp(among) - 63);
     {  // bins of the row
       constexpr int NG = kRowThreads / kLogitBins;
       const int g = tid & (kLogitBins - 1), grp = tid / kLogitBins;
@@ -579,7 +583,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
         const float v = logit(i);
         return usable(v) ? order_key(v) : 0u;
       };
-      const int wide_sum = in_lds ? 0 : 8;  // sums over a whole row: 2^20 weights fit 62 bits
+      const int wide_sum = in_lds ? 0 : wide;
       unsigned common = 0;
       int bits = 32;
       if (phase == 2) {
@@ -594,7 +598,7 @@ __global__ void __launch_bounds__(kRowThreads) k_sample_row(harli_sample_batch a
       }
       if (phase == 0 && in_lds) want -= sh.found_above;
       if (phase == 1) {
-        const double x = in_lds ? ceil(want_d - (bin ? sh.upto_weight[bin - 1] : 0.0)) : ceil(want_d / 256);
+        const double x = in_lds ? ceil(want_d - (bin ? sh.upto_weight[bin - 1] : 0.0)) : ceil(__builtin_amdgcn_ldexp(want_d, -wide));
         want = x < 1.0 ? 1 : (u64)x;
       }
       const unsigned key = common + find_key(

@@ -222,3 +222,57 @@ def test_two_streams_with_workspaces_apart():
     torch.cuda.synchronize()
     for token, _, _ in outs:
         assert np.array_equal(token.cpu().numpy(), want[0])
+
+
+# ---- top-p where a row's tokens are too many to list, against running sums over the whole row
+def tokens_at(row, uniform, tol, temperature=1.0, top_k=0, top_p=1.0):
+    """What the definition draws when the weight that top-p asks for is off by up to `tol` (of the largest weight's) and the random number
+    by 1e-9: tokens at the borders of both."""
+    z = row.astype(np.float64)
+    order = np.argsort(-z, kind="stable")
+    if 0 < top_k < len(z):
+        order = order[:top_k]
+    w = np.exp((z[order] - z[order[0]]) / temperature)
+    upto = np.cumsum(w.astype(np.longdouble))
+    got = set()
+    for e in (-tol, 0.0, tol):
+        m = len(order) if top_p >= 1 else 1 + int(np.count_nonzero(upto[:-1] < top_p * upto[-1] + e))
+        index = np.sort(order[:m])
+        run = np.cumsum(np.exp((z[index] - z[order[0]]) / temperature).astype(np.longdouble))
+        for d in (-1e-9, 0.0, 1e-9):
+            got.add(int(index[-1 if uniform >= 1 else min(int(np.searchsorted(run, max(uniform + d, 0.0) * run[-1], "right")), m - 1)]))
+    return got
+
+
+@pytest.mark.parametrize("level", [-8.0, -20.0, -25.0])
+@pytest.mark.parametrize("V", [20000, 1 << 17, 1 << 20])
+def test_top_p_inside_a_tail_of_light_tokens(level, V):
+    """A heavy token and a tail that weighs little, all of it in a few bins (or below them): top-p close to 1 ends inside the tail.  The
+    last token kept is drawn with a random number of 1.  Weights are off by at most 2^-51 each from rounding to fixed point and by 2^-44
+    of themselves, sums of them by as much."""
+    z = np.full((6, V), np.float32(level))
+    z -= np.float32(np.spacing(np.float32(abs(level)))) * (np.arange(V) // 8).astype(np.float32)
+    z[:, 0] = 0
+    tail = np.exp(z[0, 1:].astype(np.float64)).sum()
+    p = np.minimum(np.float32(1 - tail / (1 + tail) * np.array([0.9, 0.7, 0.5, 0.3, 0.1, 0.02])), np.nextafter(np.float32(1), np.float32(0)))
+    token, _ = sample(z, np.ones(6), top_p=p)
+    tol = V * 2.0 ** -51 + 2.0 ** -44 * (1 + tail)
+    for b in range(6):
+        near = tokens_at(z[b], 1.0, tol, top_p=float(p[b]))
+        assert min(near) <= int(token[b]) <= max(near), (b, int(token[b]), near)
+
+
+@pytest.mark.parametrize("spread", [0.01, 0.3, 1.0, 20.0])
+def test_top_p_and_top_k_of_flat_and_steep_rows(spread):
+    z, r = rows(6, 50257, 12, spread)
+    t = np.array([0.05, 1.0, 1.0, 3.0, 1.0, 0.3], np.float32)
+    k = np.array([0, 0, 20000, 50000, 1000, 45000])
+    for p in (0.1, 0.9, 0.999, 1 - 2.0 ** -20, 1 - 2.0 ** -24):
+        u = r.random(6).astype(np.float32)
+        token, _ = sample(z, u, temperature=t, top_k=k, top_p=np.full(6, p))
+        plain, _ = sample(z, u, temperature=t, top_p=np.full(6, p))
+        for b in range(6):
+            total = float(np.exp((z[b].astype(np.float64) - z[b].max()) / float(t[b])).sum())
+            tol = 50257 * 2.0 ** -51 + 2.0 ** -43 * total
+            assert int(token[b]) in tokens_at(z[b], float(u[b]), tol, float(t[b]), int(k[b]), float(np.float32(p))), (p, b)
+            assert int(plain[b]) in tokens_at(z[b], float(u[b]), tol, float(t[b]), 0, float(np.float32(p))), (p, b)
