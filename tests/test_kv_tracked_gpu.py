@@ -297,3 +297,24 @@ def test_a_budget_for_longer_sequences_than_an_eviction_takes_is_refused():
     args, w, m, ft, pool, ctx, ft_step, sizes, keep = small()
     with pytest.raises(ValueError):
         serve.DecodeServer(ctx, pool, m, max_batch=1, max_len=(1 << 18) + 1, stream=torch.cuda.Stream(), budget=serve.KvBudget(keep=40))
+
+
+@pytest.mark.parametrize("heads,batch", [((28, 4, 128), 48), ((5, 1, 128), 190)], ids=str)
+def test_uneven_batches_of_groups_on_the_matrix_units_take_the_list_of_chunks(heads, batch):
+    w = wl.workload(0)
+    m = dataclasses.replace(w.model, dtype="bf16", n_layers=1, n_q=heads[0], n_kv=heads[1], head_dim=heads[2], hidden=256, ffn=320)
+    lengths = np.asarray([3000] + [1 + 3 * (i % 60) for i in range(batch - 1)], np.int32)
+    case = DecodeCase(w, m, lengths)
+    assert -(-3001 // 128) * batch * m.n_kv > 4096 and batch * 3001 * m.n_kv * 128 * 4 > 256 << 20
+    track, ws = records_of(case)
+    case.ctx.kv_record_init(batch=case.B, n_tokens=case.kv_len_dev, page_table=case.table_dev, max_pages=case.max_pages, max_kv_len=3000, track=track)
+    torch.cuda.synchronize()
+    before = host(track)
+    y = torch.empty(case.B, m.hidden, device=DEV)
+    case.ctx.decode_step_tracked(batch=case.B, kv_len=case.kv_len_dev, page_table=case.table_dev, max_pages=case.max_pages, max_kv_len=3001,
+                                 x_in=case.x_dev, x_out=y, track=track, workspace=ws)
+    torch.cuda.synchronize()
+    case.ctx.check()
+    ref, weights = oracle_step(case, case.img0, case.x_np, lengths, case.table, lengths, before, 1.0)
+    assert_close(y.cpu().numpy(), ref, "hidden state")
+    check_weights(host(track), weights, lengths, case.table, lengths, {})
