@@ -297,10 +297,11 @@ size_t harli_decode_step_static_bytes(const harli_ctx* c, int32_t batch, int32_t
  *   record  = (accumulated weight, rotary position) of one token in one KV head of one layer.  Records lie in the caller's
  *             array [n_layers][page ids of the pool][n_kv_heads][page_tokens], found through the page table like keys and
  *             values (page ids: 0 .. harli_pool_stats_t.n_chunks * pages_per_block - 1).
- * These calls take their scratch memory from the caller and use nothing of the context that a step in another stream
- * writes: calls on different streams may overlap when their page tables share no page and their workspaces are apart.  In
- * one call, too, every page belongs to one sequence: no page id appears twice in the table.  They can be captured
- * into a HIP graph (the host values in the structs are part of the capture).
+ * harli_kv_attend, harli_kv_record_init and harli_kv_evict take their scratch memory from the caller and use nothing of the
+ * context that a step in another stream writes: calls on different streams may overlap when their page tables share no page
+ * and their workspaces are apart.  harli_decode_step_tracked also uses the context's own buffers, as harli_decode_step does:
+ * no two steps of a context may overlap.  In one call, too, every page belongs to one sequence: no page id appears twice in
+ * the table.  They can be captured into a HIP graph (the host values in the structs are part of the capture).
  * ======================================================================== */
 typedef struct {
   float weight;
@@ -320,7 +321,8 @@ typedef struct {
  *   P_h = softmax_j(q_h . k_j / sqrt(head_dim)),  out_h = sum_j P_hj v_j                      for j < n = n_tokens[b]
  *   weight_j <- decay * weight_j + sum of P_hj over the query heads h of the KV head           for j < n - 1
  *   the record of token n - 1 is written anew: (sum of P_h,n-1, position)
- * n = 0: out is zero and no record changes.  Records of other tokens are left as they are.  With decay = 0 the weights that
+ * n = 0: out is zero and no record changes.  Where no token of a sequence has a weight (bad pages, scores of -inf alone) out
+ * and the weights of this step are zero too.  Records of other tokens are left as they are.  With decay = 0 the weights that
  * were there are not looked at.  q is already rotated; keys and values are found as harli_decode_step leaves them.  A token of
  * a page id outside the pool (or -1) gets no weight and is reported by harli_ctx_check, as is a sequence longer than max_kv_len
  * (rounded up to whole chunks of 128 or 256 tokens) or its table row, whose further tokens are not seen. */
@@ -378,7 +380,8 @@ harli_status harli_kv_evict(harli_ctx* c, const harli_evict_batch* b, void* hip_
 
 /* ======================================================================== *
  * A token per row of logits, from random numbers the caller gives (what a service needs in place of next_token).
- * Row b, its tokens in the order of (higher logit, lower index), weights w_i = exp((logit_i - max) / temperature) in 64 bits:
+ * Row b, its tokens in the order of (higher logit, lower index), weights w_i = exp((logit_i - max) / temperature), computed in
+ * 64 bits to 2^-44 of themselves:
  *   top-k   keeps the first k;
  *   top-p   keeps, of those, each one for which the weights before it add up to less than p times the weight of the k;
  *   min-p   keeps w_i >= min_p (times the largest weight, which is 1);

@@ -1,11 +1,13 @@
 // Attention of one new token per sequence that records the weight of every cached token (harli_kv_attend and tracked decode
-// steps; Harli Sec. 2.1 decode, Sec. 4.1 index-based KV).  Two launches: the cache is read once in chunks of tokens, each leaving
+// steps; Harli Sec. 2.1 decode, Sec. 4.1 index-based KV).  Two launches: the cache is read in chunks of tokens, each leaving
 // (maximum, sum, output) and its scores; then k_attend_finish joins the chunks and turns the scores into weights, which it can
-// only now that the maximum and the sum over all chunks are known:  P_j = exp2(s_j - M) / L.
+// only now that the maximum and the sum over all chunks are known:  P_j = exp2(s_j - M) / L.  On bf16 storage a workgroup has all query
+// heads of its KV head and the cache is read once; on fp32 it has one query head, and a group's heads read the same keys and values.
 // What bounds it: HBM, for keys and values (2 d e bytes per token and KV head).  The scores are 4 bytes per token and query head,
-// written once and read back from the caches, and the records 8 + 8 bytes per token and KV head.  Of bf16 caches, first and second launch:
-// 16 sequences of 1024 tokens, 32 KV heads 46.7 and 8.0 us (273 MB, 5.9 TB/s in the first); one of 32001, 32 / 8 heads 41.5 and 10.0
-// (131 MB: a launch that fills and drains the chip once); 192 uneven ones of about 800, 28 / 4 heads 90.6 and 26.6 (377 MB).
+// written once and read back, and the records 8 + 8 bytes per token and KV head.  Of bf16 caches, first and second launch, and what the
+// first reads and writes: 16 sequences of 1024 tokens, 32 KV heads 46.9 and 8.0 us (273 MB, 5.8 TB/s); one of 32001, 32 / 8 heads 31.2
+// and 10.2 (140 MB, 4.5 TB/s: a launch that fills and drains the chip once); 192 uneven ones of about 800, 28 / 4 heads 90.1 and
+// 26.5 (383 MB, 39 of them scores and outputs of chunks, 4.3 TB/s).
 #include <algorithm>
 #include <cmath>
 
@@ -22,8 +24,8 @@ constexpr int kMostPages = 1 << 26;  // of a table row: token indexes stay in 32
 constexpr int kChunkF32 = 256;       // tokens per chunk on fp32 storage: one per thread
 constexpr int kFinishTokens = 1024;  // tokens of a block of records: four per thread
 constexpr int kPiece = 64;           // elements of an output row that are joined at a time
-// up to here an output element is one thread's (64 sequences of 200 tokens, 28 / 4 heads: 20.3 us instead of 23.6; 16 of 4096, 32 chunks,
-// 32 / 8 heads: 84.0 instead of 83.2)
+// up to here an output element is one thread's (64 sequences of 200 tokens, 28 / 4 heads: 19.8 us instead of 23.2; 16 of 4096, 32 chunks,
+// 32 / 8 heads: 66 either way)
 constexpr int kFewChunks = 16;
 
 // fp32 storage: one chunk of one query head; a thread scores one token, then a wave adds up P.V of every fourth token with a lane
@@ -323,9 +325,9 @@ void attend_finish(harli_ctx* c, const AttendWs& att, const int* kv_len, const i
   const harli_model_cfg& m = c->cfg;
   // Workgroups of a KV head: one per block of records as far as the chip holds them, and for the output rows two per CU.  In us for the
   // whole call, bf16, heads of 128: 32 sequences of about 3000 tokens, 28 / 4 heads, 1 / 4 / as many parts as there are blocks (8):
-  // 66.3 / 61.4 / 58.9; 192 of about 800, the longest 3076, 1 / 2 / 4: 120 / 111 / 109; one of 32001, 32 / 8 heads, 1 / 4 / 32: 50.7 /
-  // 50.2 / 50.0.  Output rows with one / two / four / sixteen workgroups per CU: 16 of 1024, 32 / 8 heads, 30.4 / 31.1 / 33.5 / 33.0;
-  // 64 of 200, 28 / 4 heads, 21.1 / 20.3 / 21.2 / 25.1.
+  // 66.3 / 61.4 / 58.9; 192 of about 800, the longest 3076, 1 / 2 / 4: 120 / 111 / 109; one of 32001, 32 / 8 heads, 8 (for the
+  // output rows alone) / 32: 45.3 / 40.3.  Output rows with one / two / four / sixteen workgroups per CU: 16 of 1024, 32 / 8 heads, 24.4 /
+  // 24.9 / 26.5 / 26.5; 64 of 200, 28 / 4 heads, 20.7 / 19.8 / 20.7 / 24.5.
   const int G = m.n_q_heads / m.n_kv_heads, blocks = att.scores ? (att.score_ld + kFinishTokens - 1) / kFinishTokens : 0;
   const int pieces = G * ((m.head_dim + kPiece - 1) / kPiece), heads = batch * m.n_kv_heads;
   const int parts = std::max({1, std::min(blocks, 16 * c->n_cu / heads), std::min(pieces, 2 * c->n_cu / heads)});

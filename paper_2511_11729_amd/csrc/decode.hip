@@ -486,8 +486,8 @@ __device__ __forceinline__ float token_lanes_sum(float s) {
 }
 
 // Waves per SIMD the register allocation aims at.  What the K/V stream reaches follows the bytes in flight per compute
-// unit (a workgroup keeps all of its CH tokens in flight): four query heads per KV head at d = 128 need 131 registers
-// left alone, three short of a fourth wave per SIMD, that is of 256 instead of 192 KiB in flight.
+// unit (a workgroup keeps all of its CH tokens in flight): four query heads per KV head at d = 128 need up to 130 registers
+// left alone, two more than four waves per SIMD leave each, that is 256 instead of 192 KiB in flight.
 template <int D, int G>
 constexpr int attn_min_waves() { return (D == 128 && G == 4) ? 4 : 1; }
 
@@ -1173,8 +1173,8 @@ namespace harli {
 int attend_chunk_bf16(int d, int G) { return attn_chunk(d, G); }
 
 // The chunks of harli_kv_attend on bf16 storage (k_attend_finish joins them).  Keys and values are nontemporal loads at every size: a
-// program reads the other layers' caches, and the weights, before it comes back to these (16 sequences of 8 KV heads, 16 to 131 MB,
-// ordinary / nontemporal: three caches in turn 19.2 / 19.3 to 55.2 / 50.0 us, one again and again 17.3 / 17.5 to 47.0 / 50.1).
+// program reads the other layers' caches, and the weights, before it comes back to these (16 sequences, 32 / 8 heads, 17 to 134 MB,
+// ordinary / nontemporal: three caches in turn 15.3 / 15.2 to 42.5 / 39.0 us, one again and again 13.8 / 13.8 to 34.9 / 37.9).
 harli_status attend_bf16(harli_ctx* c, const harli_attend_batch* b, const AttendWs& att, hipStream_t st) {
   AttnList list{};
   list.chunk = att.chunk;

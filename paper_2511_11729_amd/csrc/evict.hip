@@ -1,8 +1,8 @@
 // Eviction from the paged KV cache by accumulated attention weight (harli_kv_evict).  Every (layer, sequence, KV head) ranks its
 // own tokens, keeps the best and moves those of them that lie behind the kept length into the slots that fell free.
 // Reads 8 bytes per token and moves whole rows of keys and values: bound by HBM where many rows move (192 sequences of about 800 tokens
-// cut to half, 759 MB in 167 us: 4.5 TB/s, a large copy reaches 4.7), by latency where few do (16 of 1040 tokens that give up a page,
-// 128 heads each: 13.7 us for 26 MB).  Only rows behind the kept length move (not
+// cut to half, 736 MB in 168 us: 4.4 TB/s, a large copy reaches 4.7), by latency where few do (16 of 1040 tokens that give up a page,
+// 64 heads each: 13.7 us for 26 MB).  Only rows behind the kept length move (not
 // everything behind the first gap, as keeping the order would): a service that gives up one page of 16 tokens at a time moves at
 // most 16 rows per head, and sources (slots >= keep) and targets (slots < keep) never meet, so rows move in any order.
 #include <algorithm>
