@@ -331,3 +331,28 @@ def test_a_value_that_is_not_a_number_reaches_its_own_element_and_a_key_its_own_
         got = rec["w"][0, page, :, slot]
         assert np.array_equal(np.isfinite(out[b]), np.isfinite(ref)) and np.array_equal(np.isposinf(out[b]), np.isposinf(ref)), b
         assert np.array_equal(np.isnan(got), np.isnan(weight)) and np.isnan(weight[:, 0]).all() == (b == 2), b
+
+
+@pytest.mark.parametrize("dtype,heads", [("bf16", (8, 2, 128)), ("bf16", (7, 1, 128)), ("bf16", (4, 4, 64)), ("f32", (6, 2, 48))], ids=str)
+@pytest.mark.parametrize("bound", [301, 2100, 20000])
+def test_a_bound_far_above_the_lengths(dtype, heads, bound):
+    run(CacheCase([300, 0, 1, 77, 129], *heads, dtype=dtype, room=bound - 300), decay=0.5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_part_of_a_batch_and_the_output_in_place_of_the_queries(dtype):
+    case = CacheCase([200, 30, 90], 8, 2, 64, dtype=dtype)
+    q = torch.from_numpy(queries(case)).to(DEV)
+    want, before = torch.empty_like(q), case.track.clone()
+    case.attend(q, want)
+    torch.cuda.synchronize()
+    track = case.track.clone()
+    case.track.copy_(before)
+    x = q.clone()
+    case.attend(x[:2], x[:2], batch=2)                           # the third sequence: rows behind the last one, left as they were
+    torch.cuda.synchronize()
+    case.ctx.check()
+    assert torch.equal(x[:2], want[:2]) and torch.equal(x[2], q[2])
+    for b, t in ((0, track), (1, track), (2, before)):
+        page, slot = case.slots(b, int(case.n[b]))
+        assert torch.equal(case.track[0, page, :, slot], t[0, page, :, slot])

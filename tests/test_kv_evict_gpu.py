@@ -182,3 +182,26 @@ def test_many_heads(dtype, heads, layers, lengths):
     case = CacheCase(lengths, *heads, dtype=dtype, layers=layers)
     assert heads[1] * layers * len(lengths) > 256
     assert run(case, [(2 * n + 2) // 3 for n in lengths], sink=2, recent=8) > 1000
+
+
+@pytest.mark.parametrize("bound", [301, 2049, 5000, 16385, 32768, 32769, 200000])
+def test_a_bound_far_above_the_lengths(bound):
+    """The bound chooses threads and where the keys are; lengths, a sequence that fits and one without tokens as usual."""
+    case = CacheCase([300, 0, 77, 16], 2, 2, 64, layers=2, room=bound - 300)
+    assert case.longest == bound
+    run(case, [100, 5, 33, 16], sink=2, recent=9)
+
+
+def test_evictions_of_apart_sequences_on_two_streams():
+    case = CacheCase([700, 1500, 64, 900], 4, 2, 128, layers=2)
+    keep = [300, 1400, 10, 450]
+    want, rec, _ = expected(case, keep, sink=1, recent=5)
+    halves = [(slice(0, 2), torch.cuda.Stream()), (slice(2, 4), torch.cuda.Stream())]
+    keep_dev = torch.tensor(keep, dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    for part, st in halves:
+        case.ctx.kv_evict(batch=2, n_tokens=case.n_dev[part], keep=keep_dev[part], page_table=case.table_dev[part], max_pages=case.max_pages,
+                          max_kv_len=case.longest, track=case.track, sink=1, recent=5, stream=st)
+    torch.cuda.synchronize()
+    case.ctx.check()
+    assert torch.equal(case.view.cpu().view(want.dtype), want) and case.got_records().tobytes() == rec.tobytes()

@@ -276,3 +276,37 @@ def test_top_p_and_top_k_of_flat_and_steep_rows(spread):
             tol = 50257 * 2.0 ** -51 + 2.0 ** -43 * total
             assert int(token[b]) in tokens_at(z[b], float(u[b]), tol, float(t[b]), int(k[b]), float(np.float32(p))), (p, b)
             assert int(plain[b]) in tokens_at(z[b], float(u[b]), tol, float(t[b]), 0, float(np.float32(p))), (p, b)
+
+
+def test_as_many_rows_as_a_call_takes():
+    B, V = 65535, 3
+    z = torch.randn(B, V, device=DEV, generator=torch.Generator(DEV).manual_seed(0))
+    token, logprob = torch.empty(B + 1, dtype=torch.int32, device=DEV), torch.empty(B, device=DEV)
+    token.fill_(-7)
+    u = (torch.arange(B, device=DEV) + 0.5) / B
+    ws = torch.empty(hb.sample_workspace_bytes(B, V), dtype=torch.uint8, device=DEV)
+    hb.sample(z, u, token, logprob=logprob, workspace=ws)
+    torch.cuda.synchronize()
+    w = torch.exp(z.double() - z.double().amax(1, keepdim=True))
+    upto = w.cumsum(1)
+    share = u.double()[:, None] * upto[:, -1:]
+    want = (upto <= share).sum(1).clamp(max=V - 1)
+    clear = ((upto - share).abs().amin(1) > 1e-9)                # (fp32 quotients of whole numbers: some lie on a border)
+    assert clear.sum() > B - 10 and torch.equal(token[:B][clear].long(), want[clear]) and int(token[B]) == -7
+    lp = torch.log(w.gather(1, token[:B, None].long()) / upto[:, -1:])[:, 0]
+    assert bool(((logprob.double() - lp).abs() <= 2.0 ** -24 * lp.abs() + 2e-9).all())
+
+
+def test_rows_past_four_billion_logits():
+    ld, V = (1 << 31) + 5, 5000
+    rows_, r = rows(3, V, 14)
+    big = torch.empty(2 * ld + V, device=DEV)
+    z = torch.as_strided(big, (3, V), (ld, 1))
+    z.copy_(torch.from_numpy(rows_))
+    settings = dict(top_k=[0, 50, 0], top_p=[0.9, 1.0, 1.0], temperature=[1.0, 0.7, 0.0])
+    u = r.random(3).astype(np.float32)
+    token, ws = torch.empty(3, dtype=torch.int32, device=DEV), torch.empty(hb.sample_workspace_bytes(3, V), dtype=torch.uint8, device=DEV)
+    dev = {k: torch.tensor(v, dtype=torch.int32 if k == "top_k" else torch.float32, device=DEV) for k, v in settings.items()}
+    hb.sample(z, torch.from_numpy(u).to(DEV), token, workspace=ws, **dev)
+    torch.cuda.synchronize()
+    assert np.array_equal(token.cpu().numpy(), sample(rows_, u, **settings)[0])
