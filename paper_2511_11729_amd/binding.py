@@ -509,13 +509,24 @@ class Context:
     def kv_evict(self, *, batch, n_tokens, keep, page_table, max_pages, max_kv_len, track, sink=0, recent=0, position=None, n_left=None,
                  stream=None) -> None:
         """Every layer and KV head of sequence b keeps its best keep[b] tokens, in its first keep[b] slots."""
-        who, each = "kv_evict", 4 * batch
         if _INT is None:
             _kinds()
-        b = _pack_evict(batch, _array(who, "n_tokens", n_tokens, _INT, each), _array(who, "keep", keep, _INT, each),
-                        _array(who, "position", position, _INT, each), _array(who, "page_table", page_table, _INT, each * max_pages),
-                        max_pages, max_kv_len, sink, recent, _array(who, "track", track, _INT, self.record_bytes),
-                        _array(who, "n_left", n_left, _INT, each))
+        # _array's first two lines for each: short evictions wait for this call (four sequences of about 96 tokens 11.4 us, with six calls 11.7)
+        kind, each, who = _INT, 4 * batch, "kv_evict"
+        b = _pack_evict(
+            batch,
+            n_tokens.data_ptr() if isinstance(n_tokens, kind) and n_tokens.nbytes >= each and n_tokens.is_contiguous()
+            else _array(who, "n_tokens", n_tokens, kind, each),
+            keep.data_ptr() if isinstance(keep, kind) and keep.nbytes >= each and keep.is_contiguous() else _array(who, "keep", keep, kind, each),
+            position.data_ptr() if isinstance(position, kind) and position.nbytes >= each and position.is_contiguous()
+            else _array(who, "position", position, kind, each),
+            page_table.data_ptr() if isinstance(page_table, kind) and page_table.nbytes >= each * max_pages and page_table.is_contiguous()
+            else _array(who, "page_table", page_table, kind, each * max_pages),
+            max_pages, max_kv_len, sink, recent,
+            track.data_ptr() if isinstance(track, kind) and track.nbytes >= self.record_bytes and track.is_contiguous()
+            else _array(who, "track", track, kind, self.record_bytes),
+            n_left.data_ptr() if isinstance(n_left, kind) and n_left.nbytes >= each and n_left.is_contiguous()
+            else _array(who, "n_left", n_left, kind, each))
         status = _lib.harli_kv_evict(self.handle, b, None if stream is None else _stream(stream))
         if status:
             _check(status)
